@@ -308,6 +308,96 @@ bm_status_t bm_cache_check_canaries(bm_cache_t* cache, int32_t* damaged /*HOST o
 bm_status_t bm_cache_count_moved_rows(bm_cache_t* cache, int32_t on);
 bm_status_t bm_cache_moved_rows(bm_cache_t* cache, uint64_t* rows /*HOST out*/, int32_t reset, void* cuda_stream);
 
+/* ==== packed caches: rows held in 4 bits (the paper has no counterpart; Sec. 1's memory budget is the reason) ====
+ * The second way to fit more samples into a budget: a pair of d = 128 takes 144 bytes in place of 512 (bf16).  A packed cache is
+ * written (quantised) as its rows arrive -- token by token, block by block, or out of the caches that an evicting prefill left --
+ * read back, and attended to.  It does not evict: rows stay where they were written.
+ *
+ * Format.  A row (one key or one value of one head, d elements) is cut into d / 32 groups of 32 consecutive elements.  With x* the
+ * first element of a group's largest magnitude:
+ *     s = fp16(x* / -8), held to +-65504      code = clamp(rint(x / s), -8, 7), ties to even, of the exact quotient (0 where s = 0)
+ *     value = code * s
+ * A group that holds a NaN or an infinity reads back as NaN throughout.  The bytes' order inside a row is the library's own.
+ *
+ * Lengths are the caller's and live on the DEVICE, one int32 per sample, so that samples may be of unequal length and a captured graph
+ * can be replayed as the caches grow.  They are read when the kernels run; a length or first row outside 0 .. capacity counts as the
+ * nearest of the two.  Index arrays need 4-byte alignment only.
+ *
+ * The general rules at the top hold, with these differences: a packed handle keeps no state that a call changes, so any threads and
+ * streams may use one at the same time; calls that write rows which another call reads or writes must be ordered by the caller, and so
+ * must be calls of bm_packed_attend that are given the same workspace (two captured graphs that were given the same one, too).  The
+ * calling thread's current device is left as it was. */
+typedef struct bm_packed bm_packed_t; /* opaque, owned by the library */
+
+typedef struct {
+  int32_t batch;        /* b                                                                 */
+  int32_t n_layers;     /* L                                                                 */
+  int32_t n_q_heads;    /* Hq                                                                */
+  int32_t n_kv_heads;   /* Hkv, must divide Hq                                               */
+  int32_t head_dim;     /* d: 64 or 128                                                      */
+  int32_t capacity;     /* rows a (sample, kv-head) cache may hold, 1 .. 2^24                */
+  int32_t queries_max;  /* largest I of any bm_packed_attend call (sizes the workspace)      */
+  int32_t dtype;        /* bm_dtype_t of q / k / v / out                                     */
+  float softmax_scale;  /* 0 selects 1/sqrt(d)                                               */
+  int32_t device;       /* CUDA device ordinal                                               */
+} bm_packed_config_t;
+
+/* Memory model: L * Hkv * R * 2 * (d / 2 + d / 16) bytes per sample, R = capacity rounded up to a multiple of 32; the arena adds 1024
+ * bytes.  bm_packed_max_batch is the largest batch whose arena fits (cfg->batch is ignored). */
+bm_status_t bm_packed_bytes_per_sample(const bm_packed_config_t* cfg /*HOST*/, size_t* bytes /*HOST out*/);
+bm_status_t bm_packed_arena_bytes(const bm_packed_config_t* cfg /*HOST*/, size_t* bytes /*HOST out*/);
+bm_status_t bm_packed_max_batch(const bm_packed_config_t* cfg /*HOST*/, size_t hbm_budget_bytes, int32_t* b /*HOST out*/);
+/* Scratch of one bm_packed_attend call of up to queries_max queries. */
+bm_status_t bm_packed_workspace_bytes(const bm_packed_config_t* cfg /*HOST*/, size_t* bytes /*HOST out*/);
+
+/* Carve `arena` (DEVICE, 256-byte aligned, >= bm_packed_arena_bytes), zero it on cuda_stream (every row reads back as zeros) and return
+ * a handle.  The arena stays the caller's and must outlive the handle. */
+bm_status_t bm_packed_create(const bm_packed_config_t* cfg /*HOST*/, void* arena /*DEVICE*/, size_t arena_bytes, void* cuda_stream,
+                             bm_packed_t** out /*HOST out*/);
+bm_status_t bm_packed_destroy(bm_packed_t* cache); /* frees the host handle only */
+
+/* Quantise the keys and values of I tokens of every sample of the range and store token i of sample s at row start[s] + i of its caches
+ * (start NULL: row i).  With counts, only the first counts[s] tokens of a sample are stored.
+ *   k, v     DEVICE, cfg.dtype, element (s, i, h, e) at s * sample_stride + i * token_stride + h * d + e
+ *   strides  HOST: {k sample, k token, v sample, v token} in elements, or NULL for contiguous [nsamples][I][Hkv][d]; not negative, and
+ *            multiples of 16 bytes
+ *   start, counts  DEVICE int32 [nsamples], or NULL
+ * Rows outside 0 .. capacity - 1 are not stored; the device status word then becomes BM_ERR_CAPACITY (bm_packed_status).  Two tokens of a
+ * call never share a row. */
+bm_status_t bm_packed_write(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const void* k, const void* v,
+                            const int64_t* strides, int32_t I, const int32_t* start, const int32_t* counts, void* cuda_stream);
+/* The same from the caches of an evicting handle: the n pairs of every cache of samples from_sample0 .. of from_layer, in storage order,
+ * become rows 0 .. n - 1 (n: bm_cache_len; nothing happens where it is 0).  Both handles need the same dtype, head_dim, n_kv_heads and
+ * device, else BM_ERR_INVALID; BM_ERR_STATE when the samples of the range hold different n or padding pairs; BM_ERR_CAPACITY when n is
+ * above the packed capacity.  The pairs' positions and scores stay in the handle that is read. */
+bm_status_t bm_packed_write_from(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const bm_cache_t* from,
+                                 int32_t from_layer, int32_t from_sample0, void* cuda_stream);
+
+/* The values that rows row0 .. row0 + rows - 1 stand for:  k_out, v_out  DEVICE [nsamples][rows][Hkv][d], cfg.dtype, contiguous.  With
+ * lens (DEVICE int32 [nsamples], or NULL) the rows at and past a sample's length come back as zeros.  0 <= row0, row0 + rows <= capacity,
+ * else BM_ERR_INVALID. */
+bm_status_t bm_packed_read(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, int32_t row0, int32_t rows,
+                           const int32_t* lens, void* k_out, void* v_out, void* cuda_stream);
+
+/* Attention of I queries per sample over its caches' values:  out = softmax(scale * q k^T) v.  lens[s] counts the rows of sample s, the
+ * I tokens' own among them (write them first): query i sees the rows j with first[s] <= j < lens[s] - (I - 1 - i).  A query that sees no
+ * row has an output of zeros; rows that it does not see may hold anything.
+ *   q        DEVICE, cfg.dtype, element (s, i, h, e) at s * sample_stride + i * token_stride + h * d + e
+ *   strides  HOST: {sample, token} in elements, as for bm_packed_write, or NULL for contiguous [nsamples][I][Hq][d]
+ *   lens     DEVICE int32 [nsamples]      first  DEVICE int32 [nsamples], or NULL for 0 (left padding)
+ *   max_len  the largest length to expect: what the work is split by, results need not have it right; 0 for the capacity
+ *   out      DEVICE [nsamples][I][Hq][d], cfg.dtype, contiguous
+ *   workspace  DEVICE, 16-byte aligned, >= bm_packed_workspace_bytes (BM_ERR_OOM)
+ * Results are the same from run to run; how sums are split, and so their rounding, depends on nsamples, I and max_len. */
+bm_status_t bm_packed_attend(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const void* q, const int64_t* strides,
+                             int32_t I, const int32_t* lens, const int32_t* first, int32_t max_len, void* out, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+
+/* Synchronise cuda_stream and read the device status word: BM_OK, BM_ERR_CAPACITY (a write met a row outside its cache), or
+ * BM_ERR_TIMEOUT (a kernel gave up a bounded wait).  bm_packed_clear_status resets it, in stream order. */
+bm_status_t bm_packed_status(bm_packed_t* cache, int32_t* device_status /*HOST out*/, void* cuda_stream);
+bm_status_t bm_packed_clear_status(bm_packed_t* cache, void* cuda_stream);
+
 /* ---- per-kernel timing (measurement aid; the paper has no counterpart) ----
  * While enabled, every kernel launch of this library is bracketed by two CUDA events on its stream.
  * bm_profile_read waits for the recorded launches of one kernel class, returns their summed duration in

@@ -18,6 +18,14 @@ from .binding import (  # noqa: F401
     max_batch,
     workspace_bytes,
 )
+from .packed import (  # noqa: F401
+    PackedCache,
+    PackedConfig,
+    packed_arena_bytes,
+    packed_bytes_per_sample,
+    packed_max_batch,
+    packed_workspace_bytes,
+)
 
 
 def __getattr__(name):

@@ -37,12 +37,19 @@ class bm_config_t(C.Structure):
                 ("std_share_permille", C.c_int32)]
 
 
+class bm_packed_config_t(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n_layers", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("capacity", C.c_int32), ("queries_max", C.c_int32), ("dtype", C.c_int32),
+                ("softmax_scale", C.c_float), ("device", C.c_int32)]
+
+
 _lib = None
 RULES = {"average": 0, "sum_recent": 1, "current_query": 2, "window_pooled": 3, "average_std": 4}
 
 # name -> (restype, argtypes); every symbol include/batchmax.h declares
 _vp, _i32, _sz = C.c_void_p, C.c_int32, C.c_size_t
 _cfgp = C.POINTER(bm_config_t)
+_pcfgp, _i64p = C.POINTER(bm_packed_config_t), C.POINTER(C.c_int64)
 SIGNATURES = {
     "bm_cache_bytes_per_sample": (_i32, [_cfgp, C.POINTER(_sz)]),
     "bm_arena_bytes": (_i32, [_cfgp, C.POINTER(_sz)]),
@@ -73,6 +80,18 @@ SIGNATURES = {
     "bm_debug_build": (_i32, []),
     "bm_selftest_row_check": (_i32, [_vp, _vp]),
     "bm_cache_check_canaries": (_i32, [_vp, C.POINTER(_i32), _vp]),
+    "bm_packed_bytes_per_sample": (_i32, [_pcfgp, C.POINTER(_sz)]),
+    "bm_packed_arena_bytes": (_i32, [_pcfgp, C.POINTER(_sz)]),
+    "bm_packed_max_batch": (_i32, [_pcfgp, _sz, C.POINTER(_i32)]),
+    "bm_packed_workspace_bytes": (_i32, [_pcfgp, C.POINTER(_sz)]),
+    "bm_packed_create": (_i32, [_pcfgp, _vp, _sz, _vp, C.POINTER(_vp)]),
+    "bm_packed_destroy": (_i32, [_vp]),
+    "bm_packed_write": (_i32, [_vp, _i32, _i32, _i32, _vp, _vp, _i64p, _i32, _vp, _vp, _vp]),
+    "bm_packed_write_from": (_i32, [_vp, _i32, _i32, _i32, _vp, _i32, _i32, _vp]),
+    "bm_packed_read": (_i32, [_vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "bm_packed_attend": (_i32, [_vp, _i32, _i32, _i32, _vp, _i64p, _i32, _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
+    "bm_packed_status": (_i32, [_vp, C.POINTER(_i32), _vp]),
+    "bm_packed_clear_status": (_i32, [_vp, _vp]),
     "bm_profile_enable": (_i32, [_i32]),
     "bm_profile_read": (_i32, [_i32, C.POINTER(C.c_float), C.POINTER(_i32)]),
     "bm_kernel_launch_count": (C.c_uint64, []),

@@ -232,6 +232,23 @@ void set_mirror(bm_cache* c, int layer, int sample0, int nsamples, int n, int cu
 
 }  // namespace
 
+namespace bm {
+int note_cuda_error(cudaError_t e) { return cuda_fail(e); }
+
+int cache_range_rows(const bm_cache* c, int layer, int sample0, int nsamples, CacheRows* out) {
+  int n = 0, curr = 0;
+  if (bm_status_t s = check_range(c, layer, sample0, nsamples, &n, &curr); s != BM_OK) return s;
+  out->dtype = c->cfg.dtype; out->head_dim = c->cfg.head_dim; out->n_kv_heads = c->cfg.n_kv_heads; out->device = c->cfg.device;
+  out->n = n;
+  out->cap = c->cap;
+  out->padded = pad_active(c, layer, sample0, nsamples, 0, 0);
+  const CacheView v = make_view(c, layer, sample0, nsamples, n, false);
+  out->k = v.k_slab;
+  out->v = v.v_slab;
+  return BM_OK;
+}
+}  // namespace bm
+
 extern "C" {
 
 bm_status_t bm_cache_bytes_per_sample(const bm_config_t* cfg, size_t* bytes) {

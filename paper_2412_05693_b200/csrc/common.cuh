@@ -6,6 +6,8 @@
 
 #include "smem_configured.h"
 
+struct bm_cache;   // (api.cu)
+
 namespace bm {
 
 // Device-side view of one layer's slabs for a contiguous range of samples (Sec. 3: one cache per
@@ -141,6 +143,15 @@ __device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.lau
 extern unsigned long long g_launch_count;
 extern thread_local int g_last_decode_path;   // (api.cu) what bm_last_decode_path reports
 inline void count_launch(int n = 1) { g_launch_count += (unsigned long long)n; }
+
+// (api.cu) for the entry points in other files: the status code of a failed launch, and where a handle's rows lie.
+int note_cuda_error(cudaError_t e);
+struct CacheRows {
+  const void *k, *v;       // [nsamples][Hkv][cap][d], the first n rows of every cache in use
+  int dtype, head_dim, n_kv_heads, device, n, cap;
+  bool padded;             // the caches hold padding pairs
+};
+int cache_range_rows(const struct ::bm_cache* c, int layer, int sample0, int nsamples, CacheRows* out);   // a bm_status_t
 
 // Optional per-launch timing: when enabled, a ProfileScope brackets a launch with two CUDA events.
 enum KernelClass { kAttnFwd = 0, kScore = 1, kEvict = 2, kDecode = 3, kNumKernelClasses = 4 };
