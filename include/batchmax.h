@@ -342,7 +342,7 @@ typedef struct {
   int32_t device;       /* CUDA device ordinal                                               */
 } bm_packed_config_t;
 
-/* Memory model: L * Hkv * R * 2 * (d / 2 + d / 16) bytes per sample, R = capacity rounded up to a multiple of 32; the arena adds 1024
+/* Memory model: L * Hkv * R * 2 * (d / 2 + d / 16) bytes per sample, R = capacity rounded up to a multiple of 32; the arena adds 256
  * bytes.  bm_packed_max_batch is the largest batch whose arena fits (cfg->batch is ignored). */
 bm_status_t bm_packed_bytes_per_sample(const bm_packed_config_t* cfg /*HOST*/, size_t* bytes /*HOST out*/);
 bm_status_t bm_packed_arena_bytes(const bm_packed_config_t* cfg /*HOST*/, size_t* bytes /*HOST out*/);

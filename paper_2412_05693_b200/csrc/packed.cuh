@@ -5,12 +5,16 @@
 // stands at -8 exactly (up to the rounding of s), which makes the step an eighth of the largest magnitude where codes of -7 .. 7
 // have a seventh.  Stored is code + 8.  A group with a NaN or an infinity has a NaN for its scale.
 //
-// Four slabs, rows of a (layer, sample, kv-head) together: codes [rows][d / 2] and scales [rows][G] of the keys, the same of the
-// values.  A row's code bytes are ordered for the fragments that mma.m16n8k16 wants of them, so that a lane fetches all its codes
-// of a row at once and unpacks two by one AND (see packed_attend.cu):
-//   keys:   the lane (r, c) of a warp, r = lane / 4, c = lane % 4, multiplies the elements 32 g + 8 c + (0 .. 7) of every group g:
-//           a 32-bit word, element i in bits 4 i.  Its G words lie together at byte c * 4 G.
-//   values: the lane (r, c) multiplies the elements 32 g + 4 r + (0 .. 3): a 16-bit half, its G halves together at byte r * 2 G.
+// Rows are stored in tiles of 32 (a cache's rows are padded to whole tiles), each tile one piece of 32 * 2 * (d / 2 + d / 16) bytes that
+// a single bulk copy fetches:
+//     key codes [32][d / 2] | key scales [32][G] | value scales, see below | value codes [32][d / 2]
+// The bytes are ordered for the fragments that mma.m16n8k16 wants, so that a lane fetches what it needs of a row at once and unpacks two
+// codes by one AND (packed_attend.cu):
+//   key codes:    the lane (r, c) of a warp, r = lane / 4, c = lane % 4, multiplies the elements 32 g + 8 c + (0 .. 7) of every group g: a
+//                 32-bit word, element i in bits 4 i.  Its G words lie together at byte c * 4 G of the row.
+//   value codes:  the lane (r, c) multiplies the elements 32 g + 4 r + (0 .. 3), a 16-bit half per row and group, of the rows
+//                 16 t + 8 p + c and + 4 together: [t][p][r][c][g][which row], 16-bit halves.
+//   value scales: of the same rows [t][c][p][g][which row].
 #pragma once
 #include <cuda_fp16.h>
 
@@ -19,19 +23,33 @@
 namespace bm {
 
 constexpr int kPackedGroup = 32;     // elements that share a scale
-constexpr int kPackedTile = 32;      // rows of one step of the attention kernel; a cache's rows are padded to a multiple
+constexpr int kPackedTile = 32;      // rows of a tile
 constexpr int kErrCapacity = 3;      // BM_ERR_CAPACITY
 
-// One layer's packed rows for a range of samples; unit = local sample * Hkv + kv-head, its rows start at unit * stride.
+// One layer's packed rows for a range of samples; unit = local sample * Hkv + kv-head, its tiles start at unit * tiles.
 struct PackedView {
-  uint8_t* k_codes;     // [units][stride][d / 2]
-  uint8_t* v_codes;
-  __half* k_scales;     // [units][stride][d / 32]
-  __half* v_scales;
+  uint8_t* data;        // [units][tiles][tile bytes]
   int32_t capacity;     // rows a cache may hold
-  int32_t stride;       // capacity, rounded up to kPackedTile
+  int32_t tiles;        // of 32 rows, per cache
   int32_t nsamples, Hq, Hkv, g;
   int32_t* status;      // device status word
+};
+
+// Bytes and places inside a tile.
+template <int D>
+struct PackedLayout {
+  static constexpr int G = D / kPackedGroup;
+  static constexpr int kCodes = kPackedTile * D / 2, kScales = kPackedTile * G * 2;
+  static constexpr int kKeyScales = kCodes, kValueScales = kCodes + kScales, kValueCodes = kCodes + 2 * kScales;
+  static constexpr int kBytes = 2 * (kCodes + kScales);
+  // byte of the value scale of group g of the tile's row
+  __host__ __device__ static constexpr int value_scale(int row, int g) {
+    return kValueScales + 2 * ((((row / 16 * 4 + row % 4) * 2 + row % 16 / 8) * G + g) * 2 + row / 4 % 2);
+  }
+  // byte of the value codes of the elements 32 g + 4 r .. + 3 of the tile's row
+  __host__ __device__ static constexpr int value_codes(int row, int g, int r) {
+    return kValueCodes + 2 * ((((row / 8 * 8 + r) * 4 + row % 4) * G + g) * 2 + row / 4 % 2);
+  }
 };
 
 // Rows to quantise: element (sample, token, head) of k starts at k + sample * sample_stride + token * token_stride + head * head_stride.
@@ -52,11 +70,12 @@ struct PackedAttend {
   const int32_t* lens;     // [nsamples] rows of every sample's caches, its own I among them
   const int32_t* first;    // [nsamples] first row that counts, or null
   void* out;               // [nsamples][I][Hq][d] contiguous
-  float* partial;          // workspace
+  void* workspace;
   float scale;
-  int32_t max_len;         // what the work is split by
+  int32_t max_len;         // the longest length to expect
 };
-size_t packed_attend_workspace(int d, int g, int queries);   // bytes for calls of up to this many queries
+// Bytes for calls of up to this many samples, kv-heads and queries.
+size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles);
 cudaError_t launch_packed_attend(int dtype, int d, const PackedView& c, const PackedAttend& a, cudaStream_t st);
 
 }  // namespace bm

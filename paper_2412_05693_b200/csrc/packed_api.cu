@@ -9,16 +9,15 @@ using namespace bm;
 
 struct bm_packed {
   bm_packed_config_t cfg;
-  int stride, g;
+  int tiles, g;
   float scale;
   int32_t* status;
-  uint8_t *k_codes, *v_codes;
-  __half *k_scales, *v_scales;
+  uint8_t* data;    // [L][b][Hkv][tiles] tiles of 32 rows
 };
 
 namespace {
 
-constexpr size_t kHeader = 1024;   // status word, alignment of the slabs
+constexpr size_t kHeader = 256;   // status word
 
 bool config_ok(const bm_packed_config_t* c, bool need_batch) {
   if (c == nullptr) return false;
@@ -33,18 +32,18 @@ bool config_ok(const bm_packed_config_t* c, bool need_batch) {
   return true;
 }
 
-int64_t padded_rows(const bm_packed_config_t* c) { return (c->capacity + kPackedTile - 1) / kPackedTile * (int64_t)kPackedTile; }
+int tiles_of(const bm_packed_config_t* c) { return (c->capacity + kPackedTile - 1) / kPackedTile; }
+size_t tile_bytes(const bm_packed_config_t* c) { return c->head_dim == 64 ? PackedLayout<64>::kBytes : PackedLayout<128>::kBytes; }
 
 // false: more than a size holds
 bool per_sample(const bm_packed_config_t* c, size_t* bytes) {
-  const size_t row = 2 * (size_t)(c->head_dim / 2 + c->head_dim / 16);
-  return !__builtin_mul_overflow((size_t)c->n_layers * (size_t)c->n_kv_heads, (size_t)padded_rows(c) * row, bytes);
+  return !__builtin_mul_overflow((size_t)c->n_layers * (size_t)c->n_kv_heads, (size_t)tiles_of(c) * tile_bytes(c), bytes);
 }
 bool arena_size(const bm_packed_config_t* c, size_t* bytes) {
   return per_sample(c, bytes) && !__builtin_mul_overflow(*bytes, (size_t)c->batch, bytes) && !__builtin_add_overflow(*bytes, kHeader, bytes);
 }
 size_t workspace_size(const bm_packed_config_t* c) {
-  return packed_attend_workspace(c->head_dim, c->n_q_heads / c->n_kv_heads, c->queries_max);
+  return packed_attend_workspace(c->head_dim, c->batch, c->n_kv_heads, c->n_q_heads / c->n_kv_heads, c->queries_max, tiles_of(c));
 }
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -78,14 +77,10 @@ bool range_ok(const bm_packed* c, int layer, int sample0, int nsamples) {
 }
 
 PackedView view_of(const bm_packed* c, int layer, int sample0, int nsamples) {
-  const size_t row = ((size_t)layer * c->cfg.batch + sample0) * c->cfg.n_kv_heads * (size_t)c->stride;
   PackedView v;
-  v.k_codes = c->k_codes + row * (c->cfg.head_dim / 2);
-  v.v_codes = c->v_codes + row * (c->cfg.head_dim / 2);
-  v.k_scales = c->k_scales + row * (c->cfg.head_dim / kPackedGroup);
-  v.v_scales = c->v_scales + row * (c->cfg.head_dim / kPackedGroup);
+  v.data = c->data + ((size_t)layer * c->cfg.batch + sample0) * c->cfg.n_kv_heads * (size_t)c->tiles * tile_bytes(&c->cfg);
   v.capacity = c->cfg.capacity;
-  v.stride = c->stride;
+  v.tiles = c->tiles;
   v.nsamples = nsamples; v.Hq = c->cfg.n_q_heads; v.Hkv = c->cfg.n_kv_heads; v.g = c->g;
   v.status = c->status;
   return v;
@@ -128,19 +123,11 @@ bm_status_t bm_packed_create(const bm_packed_config_t* cfg, void* arena, size_t 
   bm_packed* c = new (std::nothrow) bm_packed();
   if (c == nullptr) return BM_ERR_OOM;
   c->cfg = *cfg;
-  c->stride = (int)padded_rows(cfg);
+  c->tiles = tiles_of(cfg);
   c->g = cfg->n_q_heads / cfg->n_kv_heads;
   c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)cfg->head_dim);
-  // slabs of whole tiles of 32 rows: multiples of 128 bytes, so the header's first 256 leave all of them aligned
-  const size_t rows = (size_t)cfg->n_layers * cfg->batch * cfg->n_kv_heads * (size_t)c->stride;
-  const size_t codes = rows * (cfg->head_dim / 2), scales = rows * (cfg->head_dim / kPackedGroup) * sizeof(__half);
-  char* p = static_cast<char*>(arena);
-  c->status = reinterpret_cast<int32_t*>(p);
-  p += 256;
-  c->k_codes = reinterpret_cast<uint8_t*>(p); p += codes;
-  c->v_codes = reinterpret_cast<uint8_t*>(p); p += codes;
-  c->k_scales = reinterpret_cast<__half*>(p); p += scales;
-  c->v_scales = reinterpret_cast<__half*>(p);
+  c->status = static_cast<int32_t*>(arena);
+  c->data = static_cast<uint8_t*>(arena) + kHeader;
   if (cudaError_t e = cudaMemsetAsync(arena, 0, need, static_cast<cudaStream_t>(cuda_stream)); e != cudaSuccess) {
     delete c;
     return status_of(e);
@@ -223,7 +210,7 @@ bm_status_t bm_packed_attend(bm_packed_t* c, int32_t layer, int32_t sample0, int
   a.I = I;
   a.lens = lens; a.first = first;
   a.out = out;
-  a.partial = static_cast<float*>(workspace);
+  a.workspace = workspace;
   a.scale = c->scale;
   a.max_len = max_len > 0 && max_len < c->cfg.capacity ? max_len : c->cfg.capacity;
   const OnDevice on(c->cfg.device);

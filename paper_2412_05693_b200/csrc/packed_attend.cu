@@ -2,23 +2,31 @@
 // 32 elements.  The I * g query rows that share a cache are the columns of
 //     S^T = K Q^T          A = codes of 16 keys x 16 elements, B = queries (16 elements x 8 columns)
 //     O^T = V^T P^T        A = codes of 16 elements x 16 keys, B = weights (16 keys x 8 columns)
-// on mma.m16n8k16 with fp16 inputs and fp32 sums.  Rows are read once, 9 bytes for 16 elements, so a step of one token is bound by HBM
-// as long as unpacking keeps up: about 1.1 instructions per element in place of the multiplications of 1 to 8 heads.
+// on warp-level MMAs with fp32 sums.  Rows are read once, 9 bytes for 16 elements, so a step of one token is bound by HBM as long as
+// unpacking keeps up, which is what everything here is about.  (Cycles a scheduler needs per operation, measured: logic on 32 bits, byte
+// permutations, conversions and fp16 arithmetic 2; mma.m16n8k16 of fp16 and mma.m16n8k32 of 8-bit integers 8; the latter of e4m3, which the
+// compiler makes of conversions and fp16 MMAs, 34; ex2 8.)
 //
 // Unpacking: the code + 8 is an integer u of 4 bits.  The word AND 0x000f000f holds two of them as the fp16 pair (u, u) * 2^-24
-// (subnormals, which the multiplication takes as they are), AND 0x00f000f0 two as u * 2^-20; a shift by 8 gives the other four.  No
-// addition takes the 8 away: sum u q = sum code q + 8 sum q, so the sums of Q.K start at -8 sum q, and P.V counts the sum of its own
-// rounded weights with one more MMA per group.  What that costs is digits: sums of up to 23 times what remains, at fp32's step.  It
-// is far below the rounding of bf16 outputs, and 30 times above that of fp32 ones (relative error 5e-6 measured), so fp32 caches take the
-// codes themselves, one fp16 addition per pair, and join P.V's sums tile by tile outside the MMA.
+// (subnormals, which the multiplication takes as they are), AND 0x00f000f0 two as u * 2^-20; a shift by 8 gives the other four.  AND
+// 0x0f0f0f0f it holds four bytes, shifted by 4 the other four: half the work, where the other side of the product can be 8-bit integers.
+// It can for up to four query rows, as two numbers each in two of the eight columns: q = 256 hi + lo, 15 bits with the sign for the row's
+// largest element.  No addition takes the 8 away: sum u q = sum code q + 8 sum q, so integer sums start at -8 sum q, fp32 ones at the sum over
+// the groups of s * (-8 sum q), one small MMA of the scales and the queries' sums; P.V counts the sum of its own rounded weights with one
+// more MMA per group.  What that costs is digits: sums of up to 23 times what remains, at fp32's step.  It is far below the rounding of bf16
+// outputs, and 30 times above that of fp32 ones (relative error 5e-6 measured), so fp32 caches take the codes themselves as fp16 numbers,
+// one fp16 addition per pair, and join P.V's sums tile by tile outside the MMA.
 //
-// Numbers: a query row is brought to a largest magnitude of 2^10 .. 2^11 by a power of two, so that bf16 values are exact in fp16 (fp32
-// values are two fp16 numbers, 22 bits, and two MMAs).  Weights are p * 2^12 (fp16, 11 bits; two numbers for fp32) times the
-// value's scale, brought to 1 .. 8 by a power of two per group and warp (f below); softmax statistics and all sums are fp32.
+// Numbers: a query row is brought to a largest magnitude of 2^13 .. 2^14 by a power of two for the integers (an element is off by 1/2, 2^-15
+// of the largest), of 2^14 .. 2^15 for fp16, where bf16 values are exact (fp32: two numbers, 22 bits).  Weights are p * 2^shift (fp16, 11
+// bits; two numbers for fp32) times the value's scale (fp32: and 2^lift, for scales far below 1); shift is 12, less where a scale of 2 or
+// more would pass fp16.  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.  Softmax statistics and all
+// sums are fp32.
 //
-// Every warp streams tiles of 32 rows of its own through its own ring of shared memory (cp.async.bulk, one mbarrier a slot) and keeps
-// its own maximum, sums and outputs: warps wait for nobody until the end, where they meet in shared memory, and CTAs that share a
-// cache in the workspace (packed_combine).
+// Work: the tiles of all caches of the call, one after another, are cut into equal runs, so that samples of unequal length cost no idle
+// SMs and few long caches are shared by all.  A run is one warp's, which streams it through a ring of shared memory (one
+// cp.async.bulk and one mbarrier per tile) and waits for nobody.  A cache that lies in one run is written out by its warp; of the others
+// the sums go to the workspace, and packed_combine_kernel joins them.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -29,16 +37,25 @@
 namespace bm {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
-constexpr int kStages = 3;
-constexpr float kShift = 12.f;                // weights are p * 2^12
-constexpr int kMaxSplitCtas = 1184;           // CTAs of a call whose caches are shared (8 per SM)
+constexpr int kWarps = 2;                     // independent of each other; one per CTA would cost 1 KB of shared memory more for each
+constexpr int kMostSms = 148;                 // that the workspace is sized for
+constexpr int kFullShift = 12;
 
 __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, const float* c) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+// a: bytes without sign, b: with
+__device__ __forceinline__ void mma_u8s8(int* d, const uint32_t* a, uint32_t b0, uint32_t b1, int even, int odd) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+      : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(even), "r"(odd));
+}
+// d = a (16 x 8) * b (8 x 8)
+__device__ __forceinline__ void mma_k8(float* d, uint32_t a0, uint32_t a1, uint32_t b) {
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%7,%7,%7};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(b), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t y;
@@ -77,8 +94,7 @@ __device__ __forceinline__ bool slot_full(uint64_t* b, uint32_t parity, int* sta
   *reinterpret_cast<volatile int*>(status) = tc::kErrTimeout;
   return false;
 }
-// n words of 32 bits at once
-template <int N>
+template <int N>   // N words of 32 bits at once
 __device__ __forceinline__ void lds(const void* p, uint32_t* w) {
   if constexpr (N == 4) {
     const uint4 v = *reinterpret_cast<const uint4*>(p);
@@ -102,6 +118,18 @@ __device__ __forceinline__ uint32_t codes(uint32_t w) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
+// x / d for 0 <= x < 2^31, 1 <= d < 2^31: with 2^(s - 1) < d <= 2^s and m = floor(2^32 (2^s - d) / d) + 1 (the round-up method of Granlund and
+// Montgomery, 1994), x / d = (mulhi(x, m) + x) >> s, which fits 32 bits for such x.
+struct FastDiv {
+  uint32_t d, m, s;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t by) : d(by), m(0), s(0) {
+    while ((1ull << s) < by) ++s;
+    m = (uint32_t)(((((1ull << s) - by) << 32) / by) + 1);
+  }
+  __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi((uint32_t)x, m) + (uint32_t)x) >> s); }
+};
+
 struct AttendArgs {
   PackedView c;
   const void* q;
@@ -110,562 +138,755 @@ struct AttendArgs {
   const int32_t* lens;
   const int32_t* first;
   void* out;
-  float* partial;
-  float mul;          // scale * log2(e)
-  int32_t splits, query_tiles;
+  float mul;              // scale * log2(e)
+  int32_t query_tiles;    // of 8 NT query rows, per cache
+  int32_t runs;           // the most there may be: one for each warp of the grid
+  int32_t slot_cols;      // query rows of a share in the workspace
+  FastDiv by_g, by_query_tiles;
+  long long* before;      // workspace: [nsamples + 1] tiles (of one kv-head and query tile) of the samples before each
+  float* partial;         // workspace: [runs][2][slot_cols][D + 4] sums of a cache's share, their maximum and sum of weights
 };
 
-// One CTA's share of one cache, for a tile of 8 NT query rows: rows [lo, hi) of the cache.  PIECES fp16 numbers per query and weight.
-template <typename T, int D, int NT>
+// NT tiles of 8 columns.  PAIR: up to four query rows as 8-bit integers, each with two columns in Q.K and one of two in P.V (the other's
+// weights are 0).
+template <typename T, int D, int NT, bool PAIR>
 struct Attend {
-  static constexpr bool kSigned = sizeof(T) == 4;   // the MMAs take codes, not codes + 8
-  static constexpr int G = D / kPackedGroup, kPieces = sizeof(T) == 4 ? 2 : 1, kCols = 8 * NT;
-  static constexpr int kCodes = kPackedTile * D / 2, kScales = kPackedTile * G * 2, kSlot = 2 * (kCodes + kScales);
-  static constexpr int kRing = kWarps * kStages * kSlot, kMerge = kWarps * 8 * D * 4;
-  static constexpr int kQuery = NT > 1 ? NT * kPieces * G * 2 * 32 * 8 : 0;   // B fragments of Q, where registers do not hold them
-  static constexpr int kSmem = (kRing > kMerge ? kRing : kMerge) + kQuery;
+  static constexpr bool kSigned = sizeof(T) == 4;   // fp32: the MMAs take codes, not codes + 8
+  static constexpr int G = D / kPackedGroup, kPieces = kSigned ? 2 : 1, kCols = PAIR ? 4 : 8 * NT;
+  static constexpr int kStages = NT == 1 ? 3 : 2, kResident = NT == 1 ? 12 : 8;   // slots of the ring, warps per SM
+  static constexpr int kQueryWords = kSigned ? 8 * G : PAIR ? 2 * G : 4 * G;   // B fragments of Q for 8 columns, words of a lane
+  static constexpr int kQuery = NT > 1 ? NT * kQueryWords * 32 * 4 : 0;        // in shared memory where registers do not hold them
+  static constexpr int kWarpBytes = kStages * PackedLayout<D>::kBytes + kQuery, kSmem = kWarps * kWarpBytes;
+  static_assert(!PAIR || (NT == 1 && !kSigned), "");
 };
 
-template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? (sizeof(T) == 4 ? 3 : 4) : 2) packed_attend_kernel(AttendArgs a) {
-  using A = Attend<T, D, NT>;
-  constexpr int G = A::G, P = A::kPieces;
+// The rows of a sample that some query sees: tiles first .. first + n - 1 of its caches.
+struct Tiles {
+  int len, lo, first, n;
+};
+__device__ __forceinline__ Tiles sample_tiles(const AttendArgs& a, int smp) {
+  Tiles t;
+  t.len = min(max(a.lens[smp], 0), a.c.capacity);
+  t.lo = a.first != nullptr ? max(a.first[smp], 0) : 0;
+  t.first = t.lo / kPackedTile;
+  t.n = t.len > t.lo ? (t.len + kPackedTile - 1) / kPackedTile - t.first : 0;
+  return t;
+}
+template <typename N>
+__device__ __forceinline__ N warp_inclusive_sum(N x, int lane) {
+#pragma unroll
+  for (int step = 1; step < 32; step *= 2) {
+    const N y = __shfl_up_sync(0xffffffffu, x, step);
+    if (lane >= step) x += y;
+  }
+  return x;
+}
+// v tiles in w <= v runs: run j has the tiles [start(j), start(j + 1)).
+struct Runs {
+  long long each;
+  int more;   // the first runs have one tile more
+  __device__ __forceinline__ Runs(long long v, int w) {
+    each = (unsigned long long)v >> 32 ? v / w : (long long)((uint32_t)v / (uint32_t)w);
+    more = (int)(v - each * w);
+  }
+  __device__ __forceinline__ long long start(int j) const { return j * each + min(j, more); }
+  __device__ __forceinline__ int of(long long tile) const {
+    const long long longer = (each + 1) * more;
+    const bool in_longer = tile < longer;
+    const long long x = in_longer ? tile : tile - longer, by = in_longer ? each + 1 : each;
+    return (in_longer ? 0 : more) + (int)((unsigned long long)(x | by) >> 32 ? x / by : (long long)((uint32_t)x / (uint32_t)by));
+  }
+};
+
+// A place in the order of the call's tiles: sample, kv-head, query tile, tile.
+struct Walk {
+  int smp, head, qt, t, n, first;
+  __device__ __forceinline__ void next_cache(const AttendArgs& a) {
+    t = 0;
+    if (++qt < a.query_tiles) return;
+    qt = 0;
+    if (++head < a.c.Hkv) return;
+    head = 0;
+    do {
+      const Tiles x = sample_tiles(a, ++smp);
+      n = x.n;
+      first = x.first;
+    } while (n == 0 && smp + 1 < a.c.nsamples);
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float x, float y, float z, float w) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w);
+  } else {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x, y), b = __floats2bfloat162_rn(z, w);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  }
+}
+
+template <typename T, int D, int NT, bool PAIR>
+__global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident / kWarps) packed_attend_kernel(AttendArgs a) {
+  using A = Attend<T, D, NT, PAIR>;
+  using L = PackedLayout<D>;
+  constexpr int G = A::G, P = A::kPieces, kStages = A::kStages, C = PAIR ? 1 : 2;   // C: columns of the sums that a lane has
   constexpr bool kSigned = A::kSigned;
-  constexpr float kEven = kSigned ? 1.f : 0x1p24f, kOdd = kSigned ? 1.f : 0x1p20f;   // what a code of the MMA's has to be multiplied by
+  constexpr float kEven = kSigned ? 1.f : 0x1p24f, kOdd = kSigned ? 1.f : 0x1p20f;   // what a code of the fp16 MMAs has to be multiplied by
+  constexpr float kKey = PAIR ? 1.f : kEven;
+  constexpr int kMagic = 0x4b400000;   // integers up to 2^22 on top of it are that much above the fp32 number 1.5 * 2^23
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ __align__(8) uint64_t bars[kWarps * kStages];
-  __shared__ float stat_m[kWarps][A::kCols], stat_l[kWarps][A::kCols];
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, r = lane / 4, c = lane % 4;
-  if (tid == 0) {
-    for (int i = 0; i < kWarps * kStages; ++i) tc::mbar_init(&bars[i], 1);
+  __shared__ __align__(8) uint64_t bars[kWarps][kStages];
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, c = lane % 4, run = blockIdx.x * kWarps + warp;
+  unsigned char* ring = smem + warp * A::kWarpBytes;
+  uint64_t* bar = bars[warp];
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) tc::mbar_init(&bar[i], 1);
     tc::mbar_fence_init();
   }
-  __syncthreads();
+  __syncwarp();
   pdl_wait();
   pdl_release();
 
-  const int split = blockIdx.x % a.splits, qt = (blockIdx.x / a.splits) % a.query_tiles;
-  const int unit = blockIdx.x / (a.splits * a.query_tiles);
-  const int smp = unit / a.c.Hkv, head = unit % a.c.Hkv, g = a.c.g, cols = a.I * g;
-  const int col0 = qt * A::kCols, cols_here = min(A::kCols, cols - col0);
-  const int len = min(max(a.lens[smp], 0), a.c.capacity);
-  const int lo = a.first != nullptr ? max(a.first[smp], 0) : 0;
-  // query i sees the rows [lo, len - (I - 1 - i)); this tile's queries are (col0 / g) .. (col0 + cols_here - 1) / g
-  const int i_last = (col0 + cols_here - 1) / g;
-  const int least = len - (a.I - 1 - col0 / g), hi = len - (a.I - 1 - i_last);
-  const int t_lo = lo / kPackedTile, tiles = hi > lo ? (hi + kPackedTile - 1) / kPackedTile - t_lo : 0;
-  const int t0 = (int)((long long)tiles * split / a.splits), t1 = (int)((long long)tiles * (split + 1) / a.splits);
-  const int mine = t1 - t0 > warp ? (t1 - t0 - warp + kWarps - 1) / kWarps : 0;   // tiles t0 + warp, + kWarps, ...
-
-  unsigned char* ring = smem + warp * kStages * A::kSlot;
-  uint64_t* bar = bars + warp * kStages;
-  const size_t row_base = (size_t)unit * a.c.stride;
-  auto issue = [&](int n) {   // the warp's n-th tile into slot n % kStages
-    const size_t row = row_base + (size_t)(t_lo + t0 + warp + n * kWarps) * kPackedTile;
-    unsigned char* slot = ring + (n % kStages) * A::kSlot;
-    uint64_t* b = bar + n % kStages;
-    tc::mbar_expect_tx(b, A::kSlot);
-    bulk_load(slot, a.c.k_codes + row * (D / 2), A::kCodes, b);
-    bulk_load(slot + A::kCodes, a.c.k_scales + row * G, A::kScales, b);
-    bulk_load(slot + A::kCodes + A::kScales, a.c.v_scales + row * G, A::kScales, b);
-    bulk_load(slot + A::kCodes + 2 * A::kScales, a.c.v_codes + row * (D / 2), A::kCodes, b);
+  // ---- this warp's run ------------------------------------------------------------------------------------------------------
+  const int cols = a.I * a.c.g, per_sample = a.c.Hkv * a.query_tiles;
+  // Lane i has the samples [i q, (i + 1) q): their tiles in all, and those before them.
+  const int ns = a.c.nsamples, each_lane = (ns + 31) / 32, mine0 = lane * each_lane;
+  auto tiles_at = [&](int smp) { return smp < ns ? sample_tiles(a, smp).n : 0; };
+  int tiles_of_lane = 0;
+#pragma unroll 4
+  for (int i = 0; i < each_lane; ++i) tiles_of_lane += tiles_at(mine0 + i);
+  const long long up_to_lane = warp_inclusive_sum((long long)tiles_of_lane, lane), total = __shfl_sync(0xffffffffu, up_to_lane, 31);
+  const long long all = total * per_sample;
+  if (run == 0) {   // for packed_combine_kernel
+    long long sum = up_to_lane - tiles_of_lane;
+    for (int smp = mine0; smp < min(mine0 + each_lane, ns); ++smp) {
+      a.before[smp] = sum;
+      sum += tiles_at(smp);
+    }
+    if (lane == 0) a.before[ns] = total;
+  }
+  const int runs = (int)min((long long)a.runs, all);
+  if (run >= runs) return;
+  const Runs cut(all, runs);
+  const long long begin = cut.start(run);
+  int left = (int)(cut.start(run + 1) - begin), to_issue = left;
+  Walk at;
+  {
+    const int src = __ffs(__ballot_sync(0xffffffffu, begin < up_to_lane * per_sample)) - 1;   // the lane whose samples `begin` falls to
+    long long before = __shfl_sync(0xffffffffu, up_to_lane - tiles_of_lane, src);
+    for (int s0 = src * each_lane;; s0 += 32) {
+      const int n = s0 + lane < (src + 1) * each_lane ? tiles_at(s0 + lane) : 0;
+      const long long up_to = before + warp_inclusive_sum(n, lane);
+      const unsigned hit = __ballot_sync(0xffffffffu, begin < up_to * per_sample);
+      if (hit != 0) {
+        const int k = __ffs(hit) - 1;
+        at.smp = s0 + k;
+        at.n = __shfl_sync(0xffffffffu, n, k);
+        at.first = sample_tiles(a, at.smp).first;
+        const long long in = begin - __shfl_sync(0xffffffffu, up_to - n, k) * per_sample;
+        const int unit = (unsigned long long)in >> 32 ? (int)(in / at.n) : (int)((uint32_t)in / (uint32_t)at.n);
+        at.t = (int)(in - (long long)unit * at.n);
+        at.head = a.by_query_tiles(unit);
+        at.qt = unit - at.head * a.query_tiles;
+        break;
+      }
+      before = __shfl_sync(0xffffffffu, up_to, 31);
+    }
+  }
+  Walk ahead = at;   // the next tile to fetch
+  const uint8_t* from = nullptr;
+  auto cache_tiles = [&](const Walk& w) {
+    return a.c.data + (((size_t)w.smp * a.c.Hkv + w.head) * a.c.tiles + w.first + w.t) * L::kBytes;
   };
-  if (lane == 0)
-    for (int n = 0; n < kStages && n < mine; ++n) issue(n);
+  from = cache_tiles(ahead);
+  auto issue = [&](int slot) {
+    if (to_issue == 0) return;
+    --to_issue;
+    if (lane == 0) {
+      tc::mbar_expect_tx(bar + slot, L::kBytes);
+      bulk_load(ring + slot * L::kBytes, from, L::kBytes, bar + slot);
+    }
+    from += L::kBytes;
+    if (++ahead.t == ahead.n && to_issue > 0) {
+      ahead.next_cache(a);
+      from = cache_tiles(ahead);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kStages; ++i) issue(i);
 
-  // ---- queries: lane (r, c) has the elements 32 g + 8 c .. + 7 of column 8 nt + r -------------------------------------------
-  uint32_t bq[NT == 1 ? P * G * 4 : 1];        // [piece][group][two k-steps][b0, b1]
-  float start[NT][G][2], colmul[NT][2];        // of columns 8 nt + 2 c, + 1
-  uint32_t* bq_smem = reinterpret_cast<uint32_t*>(smem + A::kSmem - A::kQuery);
+  int slot = 0;
+  uint32_t parity = 0;
+#pragma unroll 1
+  while (left > 0) {
+    // ---- one cache's share: its queries, lane (r, c) has the elements 32 g + 8 c .. + 7 of column 8 nt + r ---------------------
+    const Tiles sample = sample_tiles(a, at.smp);
+    const int len = sample.len, lo = sample.lo, share = min(at.n - at.t, left), col0 = at.qt * A::kCols;
+    const int cols_here = min(A::kCols, cols - col0);
+    // query i sees the rows [lo, len - (I - 1 - i)); the first of this tile's the rows below `least`, the last those below `most_rows`
+    const int least = len - (a.I - 1 - a.by_g(col0)), most_rows = len - (a.I - 1 - a.by_g(col0 + cols_here - 1));
+    uint32_t bq[NT == 1 ? A::kQueryWords : 1];   // [number][group][two k-steps][b0, b1], integers: [group][b0, b1]
+    uint32_t* bq_smem = reinterpret_cast<uint32_t*>(ring + kStages * L::kBytes);   // [nt][pair of words][lane][2]
+    uint32_t start[NT];                          // B fragment of the -8 sum q: two fp16 numbers for each group
+    int start_int[PAIR ? G : 1][2];              // -8 sum of hi, of lo, of this lane's column
+    float colmul[NT][C];                         // of this lane's columns
+    [[maybe_unused]] float not_finite = 0.f;     // integers: NaN where the column's query is not finite
+    auto put_query = [&](int nt, int k, uint32_t w) {
+      if constexpr (NT == 1) bq[k] = w;
+      else bq_smem[((nt * (A::kQueryWords / 2) + k / 2) * 32 + lane) * 2 + k % 2] = w;
+    };
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int col = col0 + 8 * nt + r;
-    float x[G][8];
-    float most = 0.f;
+    for (int nt = 0; nt < NT; ++nt) {
+      const int col = col0 + (PAIR ? r / 2 : 8 * nt + r), query = a.by_g(col);
+      const T* q = static_cast<const T*>(a.q) + at.smp * a.q_sample + query * a.q_token + ((size_t)at.head * a.c.g + col - query * a.c.g) * D + 8 * c;
+      float x[G][8];
+      uint32_t most_bits = 0;   // magnitudes compare as integers, what is not finite above the rest
 #pragma unroll
-    for (int gi = 0; gi < G; ++gi) {
+      for (int gi = 0; gi < G; ++gi) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[gi][j] = 0.f;
-      if (col < cols) {
-        const T* p = static_cast<const T*>(a.q) + smp * a.q_sample + (col / g) * a.q_token + ((size_t)head * g + col % g) * D + 32 * gi + 8 * c;
-        if constexpr (sizeof(T) == 2) {
-          Elem<T>::unpack(ld_global_16(p), x[gi]);
-        } else {
-          Elem<T>::unpack(ld_global_16(p), x[gi]);
-          Elem<T>::unpack(ld_global_16(p + 4), x[gi] + 4);
+        for (int j = 0; j < 8; ++j) x[gi][j] = 0.f;
+        if (col < cols) {
+          Elem<T>::unpack(ld_global_16(q + 32 * gi), x[gi]);
+          if constexpr (kSigned) Elem<T>::unpack(ld_global_16(q + 32 * gi + 4), x[gi] + 4);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most_bits = max(most_bits, __float_as_uint(x[gi][j]) & 0x7fffffffu);
+      }
+      most_bits = max(most_bits, __shfl_xor_sync(0xffffffffu, most_bits, 1));
+      most_bits = max(most_bits, __shfl_xor_sync(0xffffffffu, most_bits, 2));
+      // the largest magnitude to its place; a row that is not finite has NaN logits
+      const bool finite = most_bits < 0x7f800000u;
+      const int e = finite && most_bits > 0 ? min((PAIR ? 13 : 14) - (int)(most_bits >> 23) + 127, 100) : 0;
+      if constexpr (PAIR) not_finite = __shfl_sync(0xffffffffu, finite ? 0.f : __int_as_float(0x7fffffff), 8 * c);
+      const float up = pow2(e);
+      const float mul = fmaxf(a.mul * kKey * pow2(-e), 0x1p-126f);   // (above 0: times -inf it stays -inf)
+      if constexpr (PAIR) {
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+          // On top of kMagic the low 16 bits are the integer y; its low byte is lo, the second one of y + 128 is hi.  b0 takes the
+          // elements 0, 2, 4, 6, b1 the others.
+          const float magic = __int_as_float(r % 2 ? kMagic : kMagic + 128);
+          const uint32_t two = r % 2 ? 0x0040u : 0x0051u;
+          int sum = 0;
+#pragma unroll
+          for (int odd = 0; odd < 2; ++odd) {
+            uint32_t y[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = __float_as_uint(fmaf(x[gi][2 * j + odd], up, magic));
+            const uint32_t b = __byte_perm(__byte_perm(y[0], y[1], two), __byte_perm(y[2], y[3], two), 0x5410);
+            put_query(nt, gi * 2 + odd, b);
+            sum = __dp4a((int)b, 0x01010101, sum);
+          }
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          start_int[gi][0] = -8 * __shfl_sync(0xffffffffu, sum, 8 * c);
+          start_int[gi][1] = -8 * __shfl_sync(0xffffffffu, sum, 8 * c + 4) + kMagic;
+        }
+      } else {
+        float sums[G];
+#pragma unroll
+        for (int gi = 0; gi < G; ++gi) {
+          float sum = 0.f;
+          float v[2][8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[0][j] = x[gi][j] * up;
+            sum += v[0][j];   // (of bf16 values fp16 has all digits that count)
+            if constexpr (P == 2) v[1][j] = v[0][j] - __half2float(__float2half_rn(v[0][j]));
+          }
+#pragma unroll
+          for (int pc = 0; pc < P; ++pc)   // the k-steps take the elements (0, 4 | 1, 5) and (2, 6 | 3, 7); codes of odd ones come 16 times as large
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float by = k % 2 ? kOdd / kEven : 1.f;
+              put_query(nt, (pc * G + gi) * 4 + k, pack(v[pc][k] * by, v[pc][k + 4] * by));
+            }
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          sums[gi] = sum * (-8.f / kKey);
+        }
+        // k = 2 c, 2 c + 1 of the start's MMA: the groups 0 .. G - 1 of the first fp16 number, then those of the second
+        start[nt] = 0;
+#pragma unroll
+        for (int k = 0; k < 2 * G; k += 2) {
+          float s0 = sums[k % G], s1 = sums[k % G + 1];
+          if (k >= G) {
+            s0 -= __half2float(__float2half_rn(s0));
+            s1 -= __half2float(__float2half_rn(s1));
+          }
+          if (c == k / 2) start[nt] = pack(s0, s1);
         }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[gi][j]));
+      for (int j = 0; j < C; ++j) colmul[nt][j] = __shfl_sync(0xffffffffu, mul, 4 * (2 * c + j));   // from this lane's column to the sums'
     }
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    // the largest magnitude to 2^10 .. 2^11; an infinite row stays so, and its logits become NaN
-    const int e = most > 0.f && most < INFINITY ? min(10 - (int)((__float_as_uint(most) >> 23) & 255u) + 127, 100) : 0;
-    const float up = pow2(e);
-    float mul = a.mul * kEven * pow2(-e);
-    float sums[G];
+    auto column = [&](int nt, int j) { return PAIR ? c : 8 * nt + 2 * c + j; };   // of the sums, from col0
+    if constexpr (NT > 1) __syncwarp();
+
+    float m[NT][C], mneg[NT][C], l[NT][C], o[NT][G][2][4], ow[NT][4];   // mneg = shift - m
 #pragma unroll
-    for (int gi = 0; gi < G; ++gi) {
-      float sum = 0.f;
-      float v[2][8];
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float y = x[gi][j] * up;
-        v[0][j] = __half2float(__float2half_rn(y));
-        sum += v[0][j];
-        if constexpr (P == 2) {
-          v[1][j] = __half2float(__float2half_rn(y - v[0][j]));
-          sum += v[1][j];
-        }
+      for (int j = 0; j < C; ++j) {
+        m[nt][j] = -INFINITY;
+        mneg[nt][j] = l[nt][j] = 0.f;
       }
 #pragma unroll
-      for (int pc = 0; pc < P; ++pc) {
-        // the k-steps take the elements (0, 4 | 1, 5) and (2, 6 | 3, 7); the codes of odd elements come 16 times as large
-        constexpr float odd = kOdd / kEven;
-        const uint32_t w[4] = {pack(v[pc][0], v[pc][4]), pack(v[pc][1] * odd, v[pc][5] * odd), pack(v[pc][2], v[pc][6]),
-                               pack(v[pc][3] * odd, v[pc][7] * odd)};
+      for (int k = 0; k < 4; ++k) ow[nt][k] = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if constexpr (NT == 1) bq[(pc * G + gi) * 4 + k] = w[k];
-          else if (warp == 0) bq_smem[((((nt * P + pc) * G + gi) * 2 + k / 2) * 32 + lane) * 2 + k % 2] = w[k];
+      for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[nt][gi][k / 4][k % 4] = 0.f;
+    }
+    int shift = kFullShift;
+    [[maybe_unused]] int lift = kSigned ? 15 : 0;   // fp32: the value scales are taken times 2^lift, so that small ones keep their second number
+    auto over_of = [](int total) { return 0x7fff7fffu - 0x00010001u * (((28 - total) << 10) - 1); };
+    uint32_t over_add = over_of(shift + lift);      // carries into bit 15 what is 2^(13 - shift - lift) or more
+
+    auto rescale_outputs = [&](int nt, const float* k) {
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < C; ++j) o[nt][gi][i / 2][2 * (i % 2) + j] *= k[j];
+    };
+    auto rescale = [&](int nt, const float* k) {   // everything that was summed with the weights
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        l[nt][j] *= k[j];
+        if constexpr (!kSigned) ow[nt][j] *= k[j];
+      }
+      rescale_outputs(nt, k);
+    };
+
+    auto tile = [&](auto masked_tag, int row0, unsigned char* in) {
+      constexpr bool kMasked = decltype(masked_tag)::value;
+
+      // ---- value scales: too large for the shift, or not finite? -------------------------------------------------------------
+      {
+        uint32_t sc[G / 2], over = 0;
+        lds<G / 2>(in + L::kValueScales + lane * 2 * G, sc);
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) over |= (sc[i] & 0x7fff7fffu) + over_add;
+        if (__any_sync(0xffffffffu, (over & 0x80008000u) != 0)) {
+          uint32_t largest = 0;
+#pragma unroll
+          for (int gi = 0; gi < G; ++gi) {   // lane = row
+            unsigned short* place = reinterpret_cast<unsigned short*>(in + L::value_scale(lane, gi));
+            const uint32_t mag = *place & 0x7fffu;
+            const uint32_t bad = __ballot_sync(0xffffffffu, mag >= 0x7c00u);
+            largest = max(largest, mag >= 0x7c00u ? 0u : mag);
+            // A group whose scale is not finite is NaN for the queries that see it and nothing for the others: its scale becomes 0 in
+            // the slot, and the group's outputs of those queries NaN.
+            if (bad != 0) {
+              if (bad >> lane & 1) *place = 0;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < C; ++j) {
+                  const int seen = len - (a.I - 1 - a.by_g(col0 + column(nt, j)));
+                  const int b0 = max(lo - row0, 0), b1 = min(seen - row0, 32);
+                  const uint32_t rows = b1 > b0 ? (0xffffffffu >> (32 - (b1 - b0))) << b0 : 0u;
+                  if (bad & rows)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[nt][gi][i / 2][2 * (i % 2) + j] = __int_as_float(0x7fffffff);
+                }
+            }
+          }
+          largest = __reduce_max_sync(0xffffffffu, largest);
+          const int next = min(shift + lift, 12 - ((int)(largest >> 10) - 15));   // the largest scale is below 2^(13 - shift - lift)
+          if (next < shift + lift) {
+            const int next_shift = min(next, kFullShift);
+            const float k = pow2(next_shift - shift), k_lift = pow2(next - next_shift - lift);
+            const float ks[2] = {k, k};
+            [[maybe_unused]] const float ks_lift[2] = {k_lift, k_lift};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              rescale(nt, ks);
+              if constexpr (kSigned) rescale_outputs(nt, ks_lift);
+#pragma unroll
+              for (int j = 0; j < C; ++j)
+                if (m[nt][j] != -INFINITY) mneg[nt][j] = (float)next_shift - m[nt][j];
+            }
+            shift = next_shift;
+            lift = next - next_shift;
+            over_add = over_of(next);
+          }
+          tc::fence_async_smem();   // (the slot is filled by an asynchronous copy again)
+          __syncwarp();
         }
       }
-      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      sums[gi] = kSigned ? 0.f * sum : sum * (-8.f / kEven);   // (a row that is not finite stays so)
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {   // from the column 8 nt + r of this lane to the columns 2 c + j of the sums
-      const int from = 4 * (2 * c + j);
-      colmul[nt][j] = __shfl_sync(0xffffffffu, mul, from);
-#pragma unroll
-      for (int gi = 0; gi < G; ++gi) start[nt][gi][j] = __shfl_sync(0xffffffffu, sums[gi], from);
-    }
-  }
-  if constexpr (NT > 1) __syncthreads();
 
-  float m[NT][2], l[NT][2], o[NT][G][2][4], ow[NT][4];
+      // ---- logits -------------------------------------------------------------------------------------------------------------
+      float s[2][NT][2][C];   // [16 keys][column tile][key + 8][column]
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    m[nt][0] = m[nt][1] = -INFINITY;
-    l[nt][0] = l[nt][1] = 0.f;
+      for (int sub = 0; sub < 2; ++sub) {
+        // the MMA's row r is the key r / 2 + 4 (r % 2), so that a lane's four keys in P.V are c, c + 4, c + 8, c + 12
+        const int key = sub * 16 + r / 2 + 4 * (r % 2);
+        uint32_t w0[G], w1[G], sc[2][G / 2];
+        lds<G>(in + key * (D / 2) + c * 4 * G, w0);
+        lds<G>(in + (key + 8) * (D / 2) + c * 4 * G, w1);
+        lds<G / 2>(in + L::kKeyScales + key * G * 2, sc[0]);
+        lds<G / 2>(in + L::kKeyScales + (key + 8) * G * 2, sc[1]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) ow[nt][k] = 0.f;
+        for (int nt = 0; nt < NT; ++nt) {
+          float first[4] = {0.f, 0.f, 0.f, 0.f};
+          if constexpr (!kSigned && !PAIR) {   // (G = 2: lanes c >= 2 multiply by 0)
+            mma_k8(first, G == 4 && (c & 1) ? sc[0][G / 2 - 1] : sc[0][0], G == 4 && (c & 1) ? sc[1][G / 2 - 1] : sc[1][0], start[nt]);
+          }
 #pragma unroll
-    for (int gi = 0; gi < G; ++gi)
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[nt][gi][k / 4][k % 4] = 0.f;
-  }
-  int f[G];                     // value scales are taken times 2^f
-  uint32_t f2[G];               // 2^f as a pair
-  float bound[G];               // the scales' magnitudes up to which f is good
+            for (int j = 0; j < C; ++j) s[sub][nt][k][j] = first[2 * k + j];
+        }
 #pragma unroll
-  for (int gi = 0; gi < G; ++gi) { f[gi] = 15; f2[gi] = 0x78007800u; bound[gi] = 0x1p-12f; }
+        for (int gi = 0; gi < G; ++gi) {
+          const float2 p0 = unpack(sc[0][gi / 2]), p1 = unpack(sc[1][gi / 2]);
+          const float s0 = gi % 2 ? p0.y : p0.x, s1 = gi % 2 ? p1.y : p1.x;
+          if constexpr (PAIR) {
+            const uint32_t a0[4] = {w0[gi] & 0x0f0f0f0fu, w1[gi] & 0x0f0f0f0fu, w0[gi] >> 4 & 0x0f0f0f0fu, w1[gi] >> 4 & 0x0f0f0f0fu};
+            int acc[4];
+            mma_u8s8(acc, a0, bq[2 * gi], bq[2 * gi + 1], start_int[gi][0], start_int[gi][1]);
+            // |sum code q| < 32 * 8 * 2^14 = 2^22
+            s[sub][0][0][0] = fmaf(s0, __int_as_float(acc[0] * 256 + acc[1]) - __int_as_float(kMagic), s[sub][0][0][0]);
+            s[sub][0][1][0] = fmaf(s1, __int_as_float(acc[2] * 256 + acc[3]) - __int_as_float(kMagic), s[sub][0][1][0]);
+          } else {
+            const uint32_t x0 = w0[gi] >> 8, x1 = w1[gi] >> 8;
+            const uint32_t a0[4] = {codes<kSigned, false>(w0[gi]), codes<kSigned, false>(w1[gi]), codes<kSigned, true>(w0[gi]),
+                                    codes<kSigned, true>(w1[gi])};
+            const uint32_t a1[4] = {codes<kSigned, false>(x0), codes<kSigned, false>(x1), codes<kSigned, true>(x0), codes<kSigned, true>(x1)};
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              auto query = [&](int k, uint32_t* b) {   // the k-th pair of words
+                if constexpr (NT == 1) { b[0] = bq[2 * k]; b[1] = bq[2 * k + 1]; }
+                else lds<2>(bq_smem + ((nt * (A::kQueryWords / 2) + k) * 32 + lane) * 2, b);
+              };
+              float acc[4] = {0.f, 0.f, 0.f, 0.f};
+              uint32_t b[2];
+#pragma unroll
+              for (int pc = 0; pc < P; ++pc) {
+                query((pc * G + gi) * 2, b);
+                mma(acc, a0, b[0], b[1], acc);
+                query((pc * G + gi) * 2 + 1, b);
+                mma(acc, a1, b[0], b[1], acc);
+              }
+#pragma unroll
+              for (int j = 0; j < C; ++j) {
+                s[sub][nt][0][j] = fmaf(s0, acc[j], s[sub][nt][0][j]);
+                s[sub][nt][1][j] = fmaf(s1, acc[2 + j], s[sub][nt][1][j]);
+              }
+            }
+          }
+        }
+      }
 
-  auto tile = [&](auto masked_tag, int row0, const unsigned char* slot) {
-    constexpr bool kMasked = decltype(masked_tag)::value;
-    const unsigned char* kc = slot;
-    const unsigned char* ks = slot + A::kCodes;
-    const unsigned char* vs = ks + A::kScales;
-    const unsigned char* vc = vs + A::kScales;
-
-    // ---- logits, in units of log2 --------------------------------------------------------------------------------------
-    float s[2][NT][4];
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+      // ---- softmax, running -----------------------------------------------------------------------------------------------------
+      bool grown = false;
+      float top[NT][C];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[sub][nt][k] = 0.f;
-      // the MMA's row r is the key r / 2 + 4 (r % 2), so that a lane's four keys in P.V are c, c + 4, c + 8, c + 12
-      const int key = sub * 16 + r / 2 + 4 * (r % 2);
-      uint32_t w0[G], w1[G], sc[2][G / 2];
-      lds<G>(kc + key * (D / 2) + c * 4 * G, w0);
-      lds<G>(kc + (key + 8) * (D / 2) + c * 4 * G, w1);
-      lds<G / 2>(ks + key * G * 2, sc[0]);
-      lds<G / 2>(ks + (key + 8) * G * 2, sc[1]);
+        for (int j = 0; j < C; ++j) {
+          if constexpr (kMasked) {
+            const int seen = len - (a.I - 1 - a.by_g(col0 + column(nt, j)));
 #pragma unroll
-      for (int gi = 0; gi < G; ++gi) {
-        const uint32_t x0 = w0[gi] >> 8, x1 = w1[gi] >> 8;
-        const uint32_t a0[4] = {codes<kSigned, false>(w0[gi]), codes<kSigned, false>(w1[gi]), codes<kSigned, true>(w0[gi]),
-                                codes<kSigned, true>(w1[gi])};
-        const uint32_t a1[4] = {codes<kSigned, false>(x0), codes<kSigned, false>(x1), codes<kSigned, true>(x0), codes<kSigned, true>(x1)};
-        const float2 p0 = unpack(sc[0][gi / 2]), p1 = unpack(sc[1][gi / 2]);
-        const float s0 = gi % 2 ? p0.y : p0.x, s1 = gi % 2 ? p1.y : p1.x;
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int row = row0 + sub * 16 + 8 * k + r / 2 + 4 * (r % 2);
+                if (row < lo || row >= seen) s[sub][nt][k][j] = -INFINITY;
+              }
+          }
+          top[nt][j] = fmaxf(fmaxf(s[0][nt][0][j], s[0][nt][1][j]), fmaxf(s[1][nt][0][j], s[1][nt][1][j])) * colmul[nt][j];
+          grown |= top[nt][j] > m[nt][j] + 2.f;
+        }
+      if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float acc[4] = {start[nt][gi][0], start[nt][gi][1], start[nt][gi][0], start[nt][gi][1]};
+          float k[C];
 #pragma unroll
-          for (int pc = 0; pc < P; ++pc) {
-            if constexpr (NT == 1) {
-              const uint32_t* b = bq + (pc * G + gi) * 4;
-              mma(acc, a0, b[0], b[1], acc);
-              mma(acc, a1, b[2], b[3], acc);
-            } else {
-              const uint32_t* b = bq_smem + ((((nt * P + pc) * G + gi) * 2) * 32 + lane) * 2;
-              uint32_t b0[2], b1[2];
-              lds<2>(b, b0);
-              lds<2>(b + 64, b1);
-              mma(acc, a0, b0[0], b0[1], acc);
-              mma(acc, a1, b1[0], b1[1], acc);
-            }
+          for (int j = 0; j < C; ++j) {
+            float t = top[nt][j];
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+            t = fmaxf(m[nt][j], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16)));
+            k[j] = m[nt][j] == t ? 1.f : exp2_approx(m[nt][j] - t);   // (both -inf: nothing seen yet)
+            m[nt][j] = t;
+            mneg[nt][j] = t == -INFINITY ? 0.f : (float)shift - t;
           }
-          s[sub][nt][0] = fmaf(s0, acc[0], s[sub][nt][0]);
-          s[sub][nt][1] = fmaf(s0, acc[1], s[sub][nt][1]);
-          s[sub][nt][2] = fmaf(s1, acc[2], s[sub][nt][2]);
-          s[sub][nt][3] = fmaf(s1, acc[3], s[sub][nt][3]);
+          rescale(nt, k);
         }
       }
-    }
-
-    // ---- softmax, running ----------------------------------------------------------------------------------------------
-    bool grown = false;
-    float top[NT][2];
+      // weights p * 2^shift: lane (r, c) ends with the column r and the keys c, c + 4 (b0) and c + 8, c + 12 (b1) of every 16
+      uint32_t w[2][NT][P][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float t = -INFINITY;
-        const int seen = kMasked ? len - (a.I - 1 - (col0 + 8 * nt + 2 * c + j) / g) : 0;
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            float& x = s[sub][nt][2 * k + j];
-            x *= colmul[nt][j];
-            if constexpr (kMasked) {
-              const int row = row0 + sub * 16 + 8 * k + r / 2 + 4 * (r % 2);
-              if (row < lo || row >= seen) x = -INFINITY;
+            float p[2] = {0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+              p[j] = exp2_approx(fmaf(s[sub][nt][k][j], colmul[nt][j], mneg[nt][j]));
+              l[nt][j] += p[j];
             }
-            t = fmaxf(t, x);
+            const uint32_t h = pack(p[0], p[1]);
+            w[sub][nt][0][k] = transpose8x8(h);
+            if constexpr (P == 2) {
+              const float2 back = unpack(h);
+              w[sub][nt][P - 1][k] = transpose8x8(pack(p[0] - back.x, p[1] - back.y));
+            }
           }
-        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
-        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
-        t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16));
-        top[nt][j] = fmaxf(m[nt][j], t);
-        grown |= top[nt][j] > m[nt][j];
-      }
-    if (__any_sync(0xffffffffu, grown)) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float k[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          k[j] = m[nt][j] == top[nt][j] ? 1.f : exp2_approx(m[nt][j] - top[nt][j]);   // (both -inf: nothing seen yet)
-          m[nt][j] = top[nt][j];
-          l[nt][j] *= k[j];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ow[nt][i] *= k[i % 2];
-#pragma unroll
-        for (int gi = 0; gi < G; ++gi)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[nt][gi][i / 4][i % 4] *= k[i % 2];
-      }
-    }
-    // weights p * 2^12: lane (r, c) ends with the query r and the keys c, c + 4 (b0) and c + 8, c + 12 (b1) of every 16
-    uint32_t w[2][NT][P][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0] - kShift, m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1] - kShift;
+
+      // ---- outputs ---------------------------------------------------------------------------------------------------------------
+      [[maybe_unused]] const float lifted = pow2(lift);
+      uint32_t v[2][2][G], sv[2][2][G];   // of the keys (c, c + 4) and (c + 8, c + 12) of every 16, a word per group
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const float p0 = exp2_approx(s[sub][nt][2 * k] - m0), p1 = exp2_approx(s[sub][nt][2 * k + 1] - m1);
-          l[nt][0] += p0;
-          l[nt][1] += p1;
-          const uint32_t h = pack(p0, p1);
-          w[sub][nt][0][k] = transpose8x8(h);
-          if constexpr (P == 2) {
-            const float2 back = unpack(h);
-            w[sub][nt][P - 1][k] = transpose8x8(pack(p0 - back.x, p1 - back.y));
-          }
+          lds<G>(in + L::kValueCodes + (((sub * 2 + k) * 8 + r) * 4 + c) * G * 4, v[sub][k]);
+          lds<G>(in + L::kValueScales + ((sub * 4 + c) * 2 + k) * G * 4, sv[sub][k]);
         }
-    }
-
-    // ---- f: every lane looks at one row's scales -----------------------------------------------------------------------
-    {
-      uint32_t sc[G / 2];
-      lds<G / 2>(vs + lane * G * 2, sc);
-      bool over = false;
-      float mag[G];
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
-        const float2 p = unpack(sc[gi / 2]);
-        mag[gi] = fabsf(gi % 2 ? p.y : p.x);
-        over |= !(mag[gi] <= bound[gi]);
+        float part[kSigned ? NT : 1][2][4];
+        if constexpr (kSigned) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[nt][i / 4][i % 4] = 0.f;
+        }
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+          const uint32_t x0 = v[sub][0][gi], x1 = v[sub][1][gi], y0 = x0 >> 8, y1 = x1 >> 8;
+          const uint32_t a0[4] = {codes<kSigned, false>(x0), codes<kSigned, true>(x0), codes<kSigned, false>(x1), codes<kSigned, true>(x1)};
+          const uint32_t a1[4] = {codes<kSigned, false>(y0), codes<kSigned, true>(y0), codes<kSigned, false>(y1), codes<kSigned, true>(y1)};
+          [[maybe_unused]] const uint32_t ones = r == gi ? 0x3c003c00u : 0u;
+          [[maybe_unused]] const uint32_t a2[4] = {ones, 0u, ones, 0u};   // row gi: the sum of the weights
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            uint32_t b[P][2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              if constexpr (P == 1) {
+                b[0][k] = mul2(w[sub][nt][0][k], sv[sub][k][gi]);
+              } else {
+                const float2 hi2 = unpack(w[sub][nt][0][k]), lo2 = unpack(w[sub][nt][P - 1][k]), s2 = unpack(sv[sub][k][gi]);
+                const float y0f = (hi2.x + lo2.x) * (s2.x * lifted), y1f = (hi2.y + lo2.y) * (s2.y * lifted);
+                b[0][k] = pack(y0f, y1f);
+                const float2 back = unpack(b[0][k]);
+                b[P - 1][k] = pack(y0f - back.x, y1f - back.y);
+              }
+            }
+            float(&to)[2][4] = *(kSigned ? &part[kSigned ? nt : 0] : &o[nt][gi]);
+#pragma unroll
+            for (int pc = 0; pc < P; ++pc) {
+              mma(to[0], a0, b[pc][0], b[pc][1], to[0]);
+              mma(to[1], a1, b[pc][0], b[pc][1], to[1]);
+              if constexpr (!kSigned) mma(ow[nt], a2, b[pc][0], b[pc][1], ow[nt]);
+            }
+          }
+        }
+        if constexpr (kSigned) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[nt][gi][i / 4][i % 4] += part[nt][i / 4][i % 4];
+        }
       }
-      if (__any_sync(0xffffffffu, over)) {
+    };
+
+#pragma unroll 1
+    for (int t = at.t; t < at.t + share; ++t) {
+      if (!slot_full(bar + slot, parity, a.c.status)) {   // gave up: what is in flight lands first, then the warp ends
+#pragma unroll 1
+        for (int k = 1; k < min(kStages, left - (t - at.t)); ++k) {
+          if (++slot == kStages) { slot = 0; parity ^= 1; }
+          slot_full(bar + slot, parity, a.c.status);
+        }
+        return;
+      }
+      const int row0 = (at.first + t) * kPackedTile;
+      unsigned char* in = ring + slot * L::kBytes;
+      if (row0 >= lo && row0 + kPackedTile <= least) tile(std::false_type{}, row0, in);
+      else if (row0 < most_rows) tile(std::true_type{}, row0, in);
+      __syncwarp();
+      issue(slot);
+      if (++slot == kStages) { slot = 0; parity ^= 1; }
+    }
+
+    // ---- the cache's share is done ------------------------------------------------------------------------------------------------
+    const bool whole = share == at.n;
+    float* to = a.partial + ((size_t)run * 2 + (at.t == 0 ? 1 : 0)) * a.slot_cols * (D + 4);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int j = 0; j < C; ++j) {
+        l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], 4);
+        l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], 8);
+        l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], 16);
+        if constexpr (PAIR)
+          if (l[nt][j] != 0.f) l[nt][j] += not_finite;   // (seen something)
+        const int cc = column(nt, j), col = col0 + cc, query = a.by_g(col);
+        const float by = (whole ? (l[nt][j] == 0.f ? 0.f : 1.f / l[nt][j]) : 1.f) * pow2(-lift);   // (a query that sees no row has a row of zeros)
+        T* out = static_cast<T*>(a.out) + (((size_t)at.smp * a.I + query) * a.c.Hq + (size_t)at.head * a.c.g + col - query * a.c.g) * D + 4 * r;
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) {
-          const uint32_t most = __reduce_max_sync(0xffffffffu, mag[gi] < INFINITY ? __float_as_uint(mag[gi]) : 0u);
-          if (__uint_as_float(most) > bound[gi]) {
-            const int next = max(-15, 127 - (int)(most >> 23));   // the largest scale to 1 .. 2
-            const float k = pow2(next - f[gi]);
-            f[gi] = next;
-            f2[gi] = pack(pow2(next), pow2(next));
-            bound[gi] = pow2(3 - next);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[nt][gi][i / 4][i % 4] *= k;
-              if (r == gi) { ow[nt][0] *= k; ow[nt][1] *= k; }
-            }
-          }
-          // A group whose scale is not finite is NaN for the queries that see it and nothing for the others: its scale becomes 0
-          // in the slot, and the group's outputs of those queries NaN.
-          const uint32_t bad = __ballot_sync(0xffffffffu, !(mag[gi] < INFINITY));
-          if (bad != 0) {
-            if (bad >> lane & 1) *reinterpret_cast<unsigned short*>(const_cast<unsigned char*>(vs) + (lane * G + gi) * 2) = 0;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int j = 0; j < 2; ++j) {
-                const int seen = len - (a.I - 1 - (col0 + 8 * nt + 2 * c + j) / g);
-                const int from = max(lo - row0, 0), to = min(seen - row0, 32);
-                const uint32_t rows = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
-                if (bad & rows)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) o[nt][gi][i / 2][2 * (i % 2) + j] = __int_as_float(0x7fffffff);
-              }
+          const float sum = kSigned ? 0.f : 8.f * __shfl_sync(0xffffffffu, ow[nt][j], 4 * gi + c);
+          const float x0 = (o[nt][gi][0][j] * kEven - sum) * by, x1 = (o[nt][gi][0][2 + j] * kOdd - sum) * by;
+          const float x2 = (o[nt][gi][1][j] * kEven - sum) * by, x3 = (o[nt][gi][1][2 + j] * kOdd - sum) * by;
+          if (cc < cols_here) {
+            if (whole) store4(out + 32 * gi, x0, x1, x2, x3);
+            else store4(to + cc * (D + 4) + 32 * gi + 4 * r, x0, x1, x2, x3);
           }
         }
-        tc::fence_async_smem();   // (the slot is filled by an asynchronous copy again)
-        __syncwarp();
+        // the weights are 2^shift times p to the maximum m
+        if (!whole && r == 0 && cc < cols_here) *reinterpret_cast<float2*>(to + cc * (D + 4) + D) = make_float2(m[nt][j] - (float)shift, l[nt][j]);
       }
     }
-
-    // ---- outputs -------------------------------------------------------------------------------------------------------
-    uint32_t v[2][4][G / 2], sv[2][4][G / 2];
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int key = sub * 16 + 4 * k + c;
-        lds<G / 2>(vc + key * (D / 2) + r * 2 * G, v[sub][k]);
-        lds<G / 2>(vs + key * G * 2, sv[sub][k]);
-      }
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi) {
-      const uint32_t half = gi % 2 ? 0x7632u : 0x5410u;
-      float part[kSigned ? NT : 1][2][4];
-      if constexpr (kSigned)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) part[nt][i / 4][i % 4] = 0.f;
-#pragma unroll
-      for (int sub = 0; sub < 2; ++sub) {
-        const uint32_t x0 = __byte_perm(v[sub][0][gi / 2], v[sub][1][gi / 2], half), x1 = __byte_perm(v[sub][2][gi / 2], v[sub][3][gi / 2], half);
-        const uint32_t y0 = x0 >> 8, y1 = x1 >> 8;
-        const uint32_t a0[4] = {codes<kSigned, false>(x0), codes<kSigned, true>(x0), codes<kSigned, false>(x1), codes<kSigned, true>(x1)};
-        const uint32_t a1[4] = {codes<kSigned, false>(y0), codes<kSigned, true>(y0), codes<kSigned, false>(y1), codes<kSigned, true>(y1)};
-        [[maybe_unused]] const uint32_t ones = r == gi ? 0x3c003c00u : 0u;
-        [[maybe_unused]] const uint32_t a2[4] = {ones, 0u, ones, 0u};   // row gi: the sum of the weights
-        const uint32_t sc[2] = {mul2(__byte_perm(sv[sub][0][gi / 2], sv[sub][1][gi / 2], half), f2[gi]),
-                                mul2(__byte_perm(sv[sub][2][gi / 2], sv[sub][3][gi / 2], half), f2[gi])};
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          uint32_t b[P][2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if constexpr (P == 1) {
-              b[0][k] = mul2(w[sub][nt][0][k], sc[k]);
-            } else {
-              const float2 hi2 = unpack(w[sub][nt][0][k]), lo2 = unpack(w[sub][nt][P - 1][k]), s2 = unpack(sc[k]);
-              const float y0f = (hi2.x + lo2.x) * s2.x, y1f = (hi2.y + lo2.y) * s2.y;
-              b[0][k] = pack(y0f, y1f);
-              const float2 back = unpack(b[0][k]);
-              b[P - 1][k] = pack(y0f - back.x, y1f - back.y);
-            }
-          }
-          float(&to)[2][4] = *(kSigned ? &part[kSigned ? nt : 0] : &o[nt][gi]);
-#pragma unroll
-          for (int pc = 0; pc < P; ++pc) {
-            mma(to[0], a0, b[pc][0], b[pc][1], to[0]);
-            mma(to[1], a1, b[pc][0], b[pc][1], to[1]);
-            if constexpr (!kSigned) mma(ow[nt], a2, b[pc][0], b[pc][1], ow[nt]);
-          }
-        }
-      }
-      if constexpr (kSigned)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[nt][gi][i / 4][i % 4] += part[nt][i / 4][i % 4];
-    }
-  };
-
-  int n = 0;
-#pragma unroll 1
-  for (; n < mine; ++n) {
-    if (!slot_full(bar + n % kStages, (n / kStages) & 1, a.c.status)) break;
-    const int row0 = (t_lo + t0 + warp + n * kWarps) * kPackedTile;
-    const unsigned char* slot = ring + (n % kStages) * A::kSlot;
-    if (row0 < lo || row0 + kPackedTile > least) tile(std::true_type{}, row0, slot);
-    else tile(std::false_type{}, row0, slot);
-    __syncwarp();
-    if (lane == 0 && n + kStages < mine) issue(n + kStages);
-  }
-#pragma unroll 1
-  for (int k = n + 1; k < min(n + kStages, mine); ++k) slot_full(bar + k % kStages, (k / kStages) & 1, a.c.status);   // a wait gave up: what is in flight lands first
-
-  // ---- the warps' results meet ---------------------------------------------------------------------------------------------
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float t = l[nt][j];
-      t += __shfl_xor_sync(0xffffffffu, t, 4);
-      t += __shfl_xor_sync(0xffffffffu, t, 8);
-      t += __shfl_xor_sync(0xffffffffu, t, 16);
-      if (r == 0) {
-        stat_m[warp][8 * nt + 2 * c + j] = m[nt][j];
-        stat_l[warp][8 * nt + 2 * c + j] = t;
-      }
-    }
-  float* merge = reinterpret_cast<float*>(smem);   // [warp][8 columns][D], over the ring
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    __syncthreads();   // (the ring, or the columns before, have been read)
-    float k[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int col = 8 * nt + 2 * c + j;
-      float top = stat_m[0][col];
-#pragma unroll
-      for (int i = 1; i < kWarps; ++i) top = fmaxf(top, stat_m[i][col]);
-      k[j] = m[nt][j] == top ? 1.f : exp2_approx(m[nt][j] - top);
-    }
-#pragma unroll
-    for (int gi = 0; gi < G; ++gi) {
-      const float down = pow2(-f[gi]) ;
-      float sum[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) sum[j] = 8.f * __shfl_sync(0xffffffffu, ow[nt][j], 4 * gi + c);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const float by = k[j] * down;
-        float4 x;
-        x.x = (o[nt][gi][0][j] * kEven - sum[j]) * by;
-        x.y = (o[nt][gi][0][2 + j] * kOdd - sum[j]) * by;
-        x.z = (o[nt][gi][1][j] * kEven - sum[j]) * by;
-        x.w = (o[nt][gi][1][2 + j] * kOdd - sum[j]) * by;
-        *reinterpret_cast<float4*>(merge + (warp * 8 + 2 * c + j) * D + 32 * gi + 4 * r) = x;
-      }
-    }
-    __syncthreads();
-    for (int i = tid; i < 8 * D / 4; i += kThreads) {
-      const int col = i / (D / 4), at = (i % (D / 4)) * 4, cc = 8 * nt + col;
-      if (cc >= cols_here) continue;
-      float top = stat_m[0][cc], sum = 0.f;
-#pragma unroll
-      for (int k2 = 1; k2 < kWarps; ++k2) top = fmaxf(top, stat_m[k2][cc]);
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k2 = 0; k2 < kWarps; ++k2) {
-        const float wm = stat_m[k2][cc];
-        sum += stat_l[k2][cc] * (wm == top ? 1.f : exp2_approx(wm - top));
-        const float4 y = *reinterpret_cast<const float4*>(merge + (k2 * 8 + col) * D + at);
-        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-      }
-      if (a.splits == 1) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // (a query that sees no row has a row of zeros)
-        T* p = static_cast<T*>(a.out) + (((size_t)smp * a.I + (col0 + cc) / g) * a.c.Hq + (size_t)head * g + (col0 + cc) % g) * D + at;
-        if constexpr (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(p) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-        } else {
-          const __nv_bfloat162 y0 = __floats2bfloat162_rn(x.x * inv, x.y * inv), y1 = __floats2bfloat162_rn(x.z * inv, x.w * inv);
-          *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
-        }
-      } else {   // [unit][query tile][split][column][D + 4]: the sums, then the maximum and the sum of the weights
-        float* p = a.partial + ((size_t)blockIdx.x * A::kCols + cc) * (D + 4);
-        *reinterpret_cast<float4*>(p + at) = x;
-        if (at == 0) *reinterpret_cast<float2*>(p + D) = make_float2(top, sum);
-      }
-    }
+    left -= share;
+    if (left > 0) at.next_cache(a);
   }
 }
 
-// Joins the shares of a cache that several CTAs had: a thread has four elements of a query row.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) packed_combine_kernel(AttendArgs a, int cols_per_tile) {
-  constexpr int kPerRow = D / 4;
-  pdl_wait();
-  const long long i = (long long)blockIdx.x * (128 / kPerRow) + threadIdx.x / kPerRow;   // (unit, column)
-  const int g = a.c.g, cols = a.I * g, at = (threadIdx.x % kPerRow) * 4;
-  if (i >= (long long)a.c.nsamples * a.c.Hkv * cols) return;
-  const int unit = (int)(i / cols), col = (int)(i % cols), qt = col / cols_per_tile;
-  const size_t step = (size_t)cols_per_tile * (D + 4);
-  const float* p = a.partial + ((size_t)(unit * (long long)a.query_tiles + qt) * a.splits * cols_per_tile + col % cols_per_tile) * (D + 4);
+// Joins the shares of the caches that several runs had, and writes the zeros of queries whose caches have no tiles.  A row is one
+// (sample, kv-head, query row): D / 4 lanes have four elements each, kGroups of such lanes every kGroups-th share.
+struct Joined {
   float top = -INFINITY, sum = 0.f;
-  for (int k = 0; k < a.splits; ++k) top = fmaxf(top, p[k * step + D]);
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k = 0; k < a.splits; ++k) {
-    const float2 st = *reinterpret_cast<const float2*>(p + k * step + D);
-    if (st.y == 0.f) continue;   // nothing seen there
-    const float by = st.x == top ? 1.f : exp2_approx(st.x - top);
-    const float4 y = *reinterpret_cast<const float4*>(p + k * step + at);
-    sum += st.y * by;
-    x.x += y.x * by; x.y += y.y * by; x.z += y.z * by; x.w += y.w * by;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(float2 st, float4 v) {
+    if (st.y == 0.f) return;   // nothing seen there
+    const float next = fmaxf(top, st.x);
+    const float k = top == next ? 1.f : exp2_approx(top - next), by = st.x == next ? 1.f : exp2_approx(st.x - next);
+    top = next;
+    sum = sum * k + st.y * by;
+    o.x = o.x * k + v.x * by; o.y = o.y * k + v.y * by; o.z = o.z * k + v.z * by; o.w = o.w * k + v.w * by;
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int smp = unit / a.c.Hkv, head = unit % a.c.Hkv;
+};
+template <typename T, int D, int kGroups>
+__global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_combine_kernel(AttendArgs a, int cols_per_tile) {
+  constexpr int kPerRow = D / 4, kRows = kGroups == 1 ? 128 / kPerRow : 1, kBatch = 4;
+  __shared__ float4 sums[kGroups][kPerRow];
+  __shared__ float2 stats[kGroups];
+  pdl_wait();
+  const int x = threadIdx.x % kPerRow, y = threadIdx.x / kPerRow;
+  const long long i = (long long)blockIdx.x * kRows + (kGroups == 1 ? y : 0);
+  const int part = kGroups == 1 ? 0 : y;
+  const int g = a.c.g, cols = a.I * g, at = x * 4;
+  if (i >= (long long)a.c.nsamples * a.c.Hkv * cols) return;   // (uniform where kGroups > 1)
+  const int unit = (int)i / cols, col = (int)i % cols, qt = col / cols_per_tile, smp = unit / a.c.Hkv, head = unit % a.c.Hkv;
+  const long long per_sample = (long long)a.c.Hkv * a.query_tiles, all = a.before[a.c.nsamples] * per_sample;
+  const long long before = a.before[smp], n = a.before[smp + 1] - before;
   T* out = static_cast<T*>(a.out) + (((size_t)smp * a.I + col / g) * a.c.Hq + (size_t)head * g + col % g) * D + at;
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(out) = make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-  } else {
-    const __nv_bfloat162 y0 = __floats2bfloat162_rn(x.x * inv, x.y * inv), y1 = __floats2bfloat162_rn(x.z * inv, x.w * inv);
-    *reinterpret_cast<uint2*>(out) = make_uint2(*reinterpret_cast<const uint32_t*>(&y0), *reinterpret_cast<const uint32_t*>(&y1));
+  if (n == 0) {
+    if (part == 0) store4(out, 0.f, 0.f, 0.f, 0.f);
+    return;
   }
+  const Runs cut(all, (int)min((long long)a.runs, all));
+  const long long begin = before * per_sample + ((long long)head * a.query_tiles + qt) * n;
+  const int j0 = cut.of(begin), j1 = cut.of(begin + n - 1);
+  if (j0 == j1) return;   // written out by its warp
+  const size_t row = (size_t)a.slot_cols * (D + 4);
+  const float* p = a.partial + (size_t)(col - qt * cols_per_tile) * (D + 4);
+  Joined mine;
+  for (int j = j0 + part; j <= j1; j += kBatch * kGroups) {
+    float2 st[kBatch];
+    float4 v[kBatch];
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int jb = j + b * kGroups;
+      const float* q = p + (size_t)(2 * (long long)jb + (jb == j0 ? 1 : 0)) * row;   // the first share begins with the cache
+      st[b] = make_float2(0.f, 0.f);
+      v[b] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (jb <= j1) {
+        st[b] = *reinterpret_cast<const float2*>(q + D);
+        v[b] = *reinterpret_cast<const float4*>(q + at);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) mine.add(st[b], v[b]);
+  }
+  if constexpr (kGroups > 1) {   // halves: a tree over the groups
+    for (int half = kGroups / 2; half > 0; half /= 2) {
+      if (y >= half && y < 2 * half) {
+        sums[y][x] = mine.o;
+        if (x == 0) stats[y] = make_float2(mine.top, mine.sum);
+      }
+      __syncthreads();
+      if (y < half) mine.add(stats[y + half], sums[y + half][x]);
+    }
+    if (y != 0) return;
+  }
+  const float inv = mine.sum == 0.f ? 0.f : 1.f / mine.sum;
+  store4(out, mine.o.x * inv, mine.o.y * inv, mine.o.z * inv, mine.o.w * inv);
 }
 
-// Query rows that a CTA takes, in units of 8.
+// Query rows that a warp takes, in units of 8.
 int column_tiles(int64_t cols) { return cols <= 8 ? 1 : cols <= 16 ? 2 : 4; }
+size_t before_bytes(int nsamples) { return ((size_t)nsamples + 1 + 31) / 32 * 32 * sizeof(long long); }
 
-int choose_splits(int64_t ctas, int max_len) {
-  const int64_t most = (max_len + kWarps * kPackedTile - 1) / (kWarps * kPackedTile);   // a tile for every warp
-  return (int)std::max<int64_t>(1, std::min<int64_t>(most, kMaxSplitCtas / std::max<int64_t>(ctas, 1)));
-}
-
-template <typename T, int D, int NT>
-cudaError_t launch_nt(const AttendArgs& args, int64_t units, int max_len, cudaStream_t st) {
-  using A = Attend<T, D, NT>;
+template <typename T, int D, int NT, bool PAIR>
+cudaError_t launch_nt(const AttendArgs& args, void* workspace, int max_len, cudaStream_t st) {
+  using A = Attend<T, D, NT, PAIR>;
   AttendArgs a = args;
-  const int64_t cols = (int64_t)a.I * a.c.g;
-  const int64_t tiles = (cols + A::kCols - 1) / A::kCols;
-  a.query_tiles = (int)tiles;
-  a.splits = choose_splits(units * tiles, max_len);
-  const int64_t ctas = units * tiles * a.splits;
-  if (ctas > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  const int64_t units = (int64_t)a.c.nsamples * a.c.Hkv, cols = (int64_t)a.I * a.c.g;
+  a.query_tiles = (int)((cols + A::kCols - 1) / A::kCols);
+  const int64_t most_tiles = units * a.query_tiles * ((max_len + kPackedTile - 1) / kPackedTile);
+  a.runs = (int)std::min<int64_t>(most_tiles, std::min(sm_count(), kMostSms) * A::kResident);
+  a.slot_cols = (int)std::min<int64_t>(A::kCols, cols);
+  a.by_g = FastDiv((uint32_t)a.c.g);
+  a.by_query_tiles = FastDiv((uint32_t)a.query_tiles);
+  a.before = static_cast<long long*>(workspace);
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + before_bytes(a.c.nsamples));
   static SmemConfigured configured;
-  if (cudaError_t err = configured.ensure(packed_attend_kernel<T, D, NT>, A::kSmem); err != cudaSuccess) return err;
-  cudaError_t err = launch_dependent(packed_attend_kernel<T, D, NT>, dim3((unsigned)ctas), dim3(kThreads), A::kSmem, st, a);
+  if (cudaError_t err = configured.ensure(packed_attend_kernel<T, D, NT, PAIR>, A::kSmem); err != cudaSuccess) return err;
+  cudaError_t err = launch_dependent(packed_attend_kernel<T, D, NT, PAIR>, dim3((a.runs + kWarps - 1) / kWarps), dim3(kWarps * 32), A::kSmem, st, a);
   count_launch();
-  if (err == cudaSuccess && a.splits > 1) {
-    const int64_t per_block = 128 / (D / 4), blocks = (units * cols + per_block - 1) / per_block;
-    err = launch_dependent(packed_combine_kernel<T, D>, dim3((unsigned)blocks), dim3(128), 0, st, a, (int)A::kCols);
-    count_launch();
+  if (err != cudaSuccess) return err;
+  const int64_t rows = units * cols;
+  const int64_t shares = a.runs / (units * a.query_tiles);   // of a cache, more or less
+  const int cols_per_tile = (int)A::kCols;
+  if (shares >= 32) {
+    constexpr int kGroups = 4096 / D;   // 1024 threads
+    err = launch_dependent(packed_combine_kernel<T, D, kGroups>, dim3((unsigned)rows), dim3(1024), 0, st, a, cols_per_tile);
+  } else if (shares >= 4) {
+    constexpr int kGroups = 1024 / D;   // 256 threads
+    err = launch_dependent(packed_combine_kernel<T, D, kGroups>, dim3((unsigned)rows), dim3(256), 0, st, a, cols_per_tile);
+  } else {
+    const int per_block = 128 / (D / 4);
+    err = launch_dependent(packed_combine_kernel<T, D, 1>, dim3((unsigned)((rows + per_block - 1) / per_block)), dim3(128), 0, st, a,
+                           cols_per_tile);
   }
+  count_launch();
   return err != cudaSuccess ? err : cudaGetLastError();
 }
 
 template <typename T, int D>
-cudaError_t launch_t(const AttendArgs& a, int64_t units, int max_len, cudaStream_t st) {
+cudaError_t launch_t(const AttendArgs& a, void* workspace, int max_len, cudaStream_t st) {
   switch (column_tiles((int64_t)a.I * a.c.g)) {
-    case 1: return launch_nt<T, D, 1>(a, units, max_len, st);
-    case 2: return launch_nt<T, D, 2>(a, units, max_len, st);
-    default: return launch_nt<T, D, 4>(a, units, max_len, st);
+    case 1:
+      if constexpr (sizeof(T) == 2)
+        if ((int64_t)a.I * a.c.g <= 4) return launch_nt<T, D, 1, true>(a, workspace, max_len, st);
+      return launch_nt<T, D, 1, false>(a, workspace, max_len, st);
+    case 2: return launch_nt<T, D, 2, false>(a, workspace, max_len, st);
+    default: return launch_nt<T, D, 4, false>(a, workspace, max_len, st);
   }
 }
 
 }  // namespace
 
-size_t packed_attend_workspace(int d, int g, int queries) {
-  // CTAs that share caches, each with up to this many query rows
-  return (size_t)kMaxSplitCtas * 8 * column_tiles((int64_t)queries * g) * (d + 4) * sizeof(float);
+size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles) {
+  // The most that a call of up to this size may take, whichever kernel column_tiles chooses for it: every run leaves two shares at most.
+  size_t most = 0;
+  for (int nt = 1; nt <= column_tiles((int64_t)queries * g); nt *= 2) {
+    const int64_t cols = std::min((int64_t)queries * g, (int64_t)(nt == 4 ? INT32_MAX : 8 * nt));
+    const int64_t all = (int64_t)batch * Hkv * ((cols + 8 * nt - 1) / (8 * nt)) * tiles;
+    most = std::max(most, (size_t)std::min(all, (int64_t)kMostSms * (nt == 1 ? 12 : 8)) * 2 * std::min<int64_t>(8 * nt, cols) * (d + 4) * sizeof(float));
+  }
+  return before_bytes(batch) + most;
 }
 
 cudaError_t launch_packed_attend(int dtype, int d, const PackedView& c, const PackedAttend& p, cudaStream_t st) {
@@ -675,12 +896,13 @@ cudaError_t launch_packed_attend(int dtype, int d, const PackedView& c, const Pa
   a.I = p.I;
   a.lens = p.lens; a.first = p.first;
   a.out = p.out;
-  a.partial = p.partial;
   a.mul = p.scale * 1.4426950408889634f;
-  a.splits = a.query_tiles = 1;
-  const int64_t units = (int64_t)c.nsamples * c.Hkv;
-  if (dtype == 0) return d == 64 ? launch_t<float, 64>(a, units, p.max_len, st) : launch_t<float, 128>(a, units, p.max_len, st);
-  return d == 64 ? launch_t<__nv_bfloat16, 64>(a, units, p.max_len, st) : launch_t<__nv_bfloat16, 128>(a, units, p.max_len, st);
+  a.query_tiles = a.runs = a.slot_cols = 1;
+  a.before = nullptr;
+  a.partial = nullptr;
+  if (dtype == 0) return d == 64 ? launch_t<float, 64>(a, p.workspace, p.max_len, st) : launch_t<float, 128>(a, p.workspace, p.max_len, st);
+  return d == 64 ? launch_t<__nv_bfloat16, 64>(a, p.workspace, p.max_len, st)
+                 : launch_t<__nv_bfloat16, 128>(a, p.workspace, p.max_len, st);
 }
 
 }  // namespace bm

@@ -100,18 +100,17 @@ __global__ void __launch_bounds__(kThreads) packed_write_kernel(PackedView c, Ro
   const float fk = __half2float(sk), fv = __half2float(sv);
   // a NaN scale: the codes do not matter, but are the same for the same rows
   const uint32_t wk = fk == fk ? quantise8(x[0], fk) : 0x88888888u, wv = fv == fv ? quantise8(x[1], fv) : 0x88888888u;
-  // values: a pair of groups exchanges halves, so that each lane writes one word (the halves of two groups)
-  const uint32_t other = __shfl_xor_sync(0xffffffffu, (group & 1) ? (wv & 0xffffu) : (wv >> 16), 4);
   if (!kept) return;
-  const size_t to = ((size_t)smp * c.Hkv + head) * c.stride + (size_t)at;
-  uint8_t* kc = c.k_codes + to * (D / 2);
-  uint8_t* vc = c.v_codes + to * (D / 2);
+  using L = PackedLayout<D>;
+  uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + (size_t)at / kPackedTile) * L::kBytes;
+  const int in = (int)(at % kPackedTile);
+  uint8_t* kc = tile + in * (D / 2);
   *reinterpret_cast<uint32_t*>(kc + quad * 4 * G + group * 4) = wk;
-  *reinterpret_cast<uint32_t*>(vc + (2 * quad + (group & 1)) * 2 * G + (group & ~1) * 2) =
-      (group & 1) ? (other | (wv & 0xffff0000u)) : ((wv & 0xffffu) | (other << 16));
+  *reinterpret_cast<uint16_t*>(tile + L::value_codes(in, group, 2 * quad)) = (uint16_t)wv;
+  *reinterpret_cast<uint16_t*>(tile + L::value_codes(in, group, 2 * quad + 1)) = (uint16_t)(wv >> 16);
   if (quad == 0) {
-    c.k_scales[to * G + group] = sk;
-    c.v_scales[to * G + group] = sv;
+    *reinterpret_cast<__half*>(tile + L::kKeyScales + (in * G + group) * 2) = sk;
+    *reinterpret_cast<__half*>(tile + L::value_scale(in, group)) = sv;
   }
 }
 
@@ -151,12 +150,14 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(PackedView c, int
   uint32_t wk = 0x88888888u, wv = 0x88888888u;
   float fk = 0.f, fv = 0.f;
   if (lens == nullptr || at < lens[smp]) {
-    const size_t from = ((size_t)smp * c.Hkv + head) * c.stride + (size_t)at;
-    wk = *reinterpret_cast<const uint32_t*>(c.k_codes + from * (D / 2) + quad * 4 * G + group * 4);
-    const uint8_t* vc = c.v_codes + from * (D / 2) + quad * 4 * G + group * 2;
-    wv = *reinterpret_cast<const uint16_t*>(vc) | ((uint32_t)*reinterpret_cast<const uint16_t*>(vc + 2 * G) << 16);
-    fk = __half2float(c.k_scales[from * G + group]);
-    fv = __half2float(c.v_scales[from * G + group]);
+    using L = PackedLayout<D>;
+    const uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + at / kPackedTile) * L::kBytes;
+    const int in = at % kPackedTile;
+    wk = *reinterpret_cast<const uint32_t*>(tile + in * (D / 2) + quad * 4 * G + group * 4);
+    wv = *reinterpret_cast<const uint16_t*>(tile + L::value_codes(in, group, 2 * quad)) |
+         ((uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_codes(in, group, 2 * quad + 1)) << 16);
+    fk = __half2float(*reinterpret_cast<const __half*>(tile + L::kKeyScales + (in * G + group) * 2));
+    fv = __half2float(*reinterpret_cast<const __half*>(tile + L::value_scale(in, group)));
   }
   store8(k_out + row * D + part * 8, wk, fk);
   store8(v_out + row * D + part * 8, wv, fv);

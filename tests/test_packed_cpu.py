@@ -24,7 +24,7 @@ def cfg(**kw):
 def test_memory_model():
     assert bm.packed_bytes_per_sample(cfg()) == 8 * 1024 * 2 * 72
     assert bm.packed_bytes_per_sample(cfg(capacity=1025, n_layers=3, head_dim=64, dtype="f32")) == 3 * 8 * 1056 * 2 * 36
-    assert bm.packed_arena_bytes(cfg()) == 1024 + 16 * 8 * 1024 * 144
+    assert bm.packed_arena_bytes(cfg()) == 256 + 16 * 8 * 1024 * 144
     for budget in (100, 3 << 30, 40 << 30):
         b = bm.packed_max_batch(cfg(), budget)
         assert (b == 0 or bm.packed_arena_bytes(cfg(batch=b)) <= budget) and bm.packed_arena_bytes(cfg(batch=b + 1)) > budget

@@ -293,6 +293,14 @@ def test_queries_that_are_not_finite_or_zero():
     mean = ref.packed_values(v)[0, :, 0].mean(0)
     wide = ref.packed_values(v)[0, :, 0].abs().mean(0)
     assert ((out[0, 0, 2:] - mean).abs() <= 2.0 ** -8 * mean.abs() + 2.0 ** -9 * wide).all()
+    # one that sees no row has a row of zeros all the same; the others of its tile are not touched by it
+    for dtype, bad in [("bf16", math.nan), ("bf16", math.inf), ("f32", math.nan)]:
+        cache = make(1, 1, 1, 64, 50, dtype, queries_max=4)
+        k, v, q = (rows(gen, 1, n, 1, 64, dtype=dtype) for n in (50, 50, 4))
+        cache.write(k, v)
+        q[0, 0, 0, 1] = q[0, 2, 0, 9] = bad
+        out = cache.attend(q, ints([40]), first=ints([38])).float().cpu()     # rows 38 .. 36, 37, 38 and 39
+        assert not out[0, :2].any() and out[0, 2].isnan().all() and not out[0, 3].isnan().any()
 
 
 def test_a_long_cache_whose_offsets_pass_32_bits():
