@@ -1,8 +1,8 @@
 // Writing rows into a packed cache, and reading them back (packed.cuh has the format).
 //
-// Both are bound by HBM: a row of d elements comes in as d * e bytes and goes out as d / 2 + d / 16, or the other way round.  A thread
-// has eight consecutive elements (one 16-byte load in bf16), four threads a group: the group's peak takes two shuffles, and every
-// word of a packed row is written by one thread.
+// Both are bound by HBM: a row of d elements comes in as d * e bytes and goes out as d / 2 + d / 16, or the other way round.  A CTA has one
+// tile of a cache, whose bytes meet in shared memory, so that global memory sees whole 16-byte pieces although a tile's bytes are ordered for
+// the attention kernel.  A thread has eight consecutive elements of a row, four threads a group.
 #include <algorithm>
 
 #include "packed.cuh"
@@ -11,173 +11,227 @@ namespace bm {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: adding it rounds to integers, ties to even; the low bits are the integer
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* x);
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* x) {
-  const uint4 a = ld_global_16(p), b = ld_global_16(p + 4);
-  Elem<float>::unpack(a, x);
-  Elem<float>::unpack(b, x + 4);
+__device__ __forceinline__ void unpack8(const uint4* raw, float* x) {
+  Elem<T>::unpack(raw[0], x);
+  if constexpr (sizeof(T) == 4) Elem<T>::unpack(raw[1], x + 4);
 }
-template <>
-__device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16* p, float* x) {
-  Elem<__nv_bfloat16>::unpack(ld_global_16(p), x);
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
 }
 
-// Code + 8 of every element: rint(x / s) of the exact quotient, ties to even.  x / s has at most 24 by 11 bits, so it is a tie or
-// at least 2^-24 of itself away from one; x * (1 / s) errs by less than 2^-22 of itself, so only quotients within 2^-18 of a
-// half-integer (|quotient| <= 8 where it is not clamped) have to be divided.
-constexpr float kNearTie = 0.5f - 0x1p-18f;
-
-__device__ __forceinline__ uint32_t quantise8(const float* x, float s) {
-  constexpr float kMagic = 12582912.f + 8.f;   // 1.5 * 2^23 + 8: adding it rounds to integers, the low bits are the code + 8
-  if (!(s != 0.f)) return 0x88888888u;
-  const float inv = __frcp_rn(s);
-  uint32_t w = 0;
-  float worst = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float t = fminf(fmaxf(x[i] * inv, -8.f), 7.f);
-    const float m = t + kMagic;
-    worst = fmaxf(worst, fabsf(t - (m - kMagic)));
-    w |= (__float_as_uint(m) & 15u) << (4 * i);
-  }
-  if (worst > kNearTie) {
-    w = 0;
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      const float m = fminf(fmaxf(__fdiv_rn(x[i], s), -8.f), 7.f) + kMagic;
-      w |= (__float_as_uint(m) & 15u) << (4 * i);
-    }
-  }
-  return w;
-}
-
-// The group's scale: four lanes with eight elements each, in order.
-__device__ __forceinline__ __half group_scale(const float* x, int c) {
-  float peak = x[0];
-  uint32_t most = __float_as_uint(x[0]) & 0x7fffffffu;
+// The group's scale: four lanes with eight elements each, in order (quad = which of the four).
+__device__ __forceinline__ __half group_scale(const float* x, int quad) {
+  float top = x[0], low = -x[0];
 #pragma unroll
   for (int i = 1; i < 8; ++i) {
-    const uint32_t m = __float_as_uint(x[i]) & 0x7fffffffu;   // magnitudes compare as integers, NaN and infinity above the rest
-    if (m > most) { most = m; peak = x[i]; }
+    top = max_nan(top, x[i]);
+    low = max_nan(low, -x[i]);
   }
 #pragma unroll
   for (int step = 1; step < 4; step *= 2) {
-    const float other = __shfl_xor_sync(0xffffffffu, peak, step);
-    const uint32_t m = __float_as_uint(other) & 0x7fffffffu;
-    if (m > most || (m == most && (c & step))) { most = m; peak = other; }   // equal: the lower elements' lane
+    top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, step));
+    low = max_nan(low, __shfl_xor_sync(0xffffffffu, low, step));
   }
-  if (most >= 0x7f800000u) return __ushort_as_half((unsigned short)0x7fff);
+  float peak = top > low ? top : -low;
+  if (__any_sync(0xffffffffu, top == low)) {   // largest magnitudes of both signs: the first one counts
+    uint32_t first = 64;                       // 2 * place, + 1 where it is negative
+#pragma unroll
+    for (int i = 7; i >= 0; --i)
+      if (fabsf(x[i]) == top) first = 2 * (8 * quad + i) + (x[i] < 0.f ? 1 : 0);
+    first = min(first, __shfl_xor_sync(0xffffffffu, first, 1));
+    first = min(first, __shfl_xor_sync(0xffffffffu, first, 2));
+    if (top == low) peak = first & 1 ? -top : top;
+  }
+  if (!(fabsf(peak) < INFINITY)) return __ushort_as_half((unsigned short)0x7fff);
   return __float2half_rn(fminf(fmaxf(peak * -0.125f, -65504.f), 65504.f));
 }
 
-// One thread: eight elements of a key row and of the value row beside it.  Row index: ((sample * I + token) * Hkv + head).
+// Codes + 8 of eight elements, element i in bits 4 i: rint(x / s) of the exact quotient, ties to even.
+template <typename T>
+__device__ __forceinline__ uint32_t quantise8(const float* x, float s) {
+  if (!(s != 0.f) || s != s) return 0x88888888u;   // (NaN: the codes do not matter, but are the same for the same rows)
+  const float inv = __frcp_rn(s);
+  uint32_t m[8];
+  if constexpr (sizeof(T) == 2) {
+    // A quotient of 8 by 11 bits is a tie or at least 2^-12 away from one, and x * inv errs by less than 2^-20.  On top of 192 fp32 has
+    // steps of 2^-16: there a tie is exact again, and everything else stays on its side.
+    constexpr float kStep = 192.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      m[i] = __float_as_uint(fminf(fmaxf(fmaf(x[i], inv, kStep), kStep - 8.f), kStep + 7.f) + (kMagic - kStep + 8.f));
+  } else {
+    // A quotient of 24 by 11 bits may be 2^-24 of itself away from a tie; x * inv errs by less than 2^-22 of itself.  Those within 2^-18 of a
+    // half-integer are divided.
+    float worst = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = fminf(fmaxf(x[i] * inv, -8.f), 7.f), k = t + (kMagic + 8.f);
+      worst = fmaxf(worst, fabsf(t - (k - (kMagic + 8.f))));
+      m[i] = __float_as_uint(k);
+    }
+    if (worst > 0.5f - 0x1p-18f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = __float_as_uint(fminf(fmaxf(__fdiv_rn(x[i], s), -8.f), 7.f) + (kMagic + 8.f));
+    }
+  }
+  const uint32_t even = __byte_perm(__byte_perm(m[0], m[2], 0x0040), __byte_perm(m[4], m[6], 0x0040), 0x5410);
+  const uint32_t odd = __byte_perm(__byte_perm(m[1], m[3], 0x0040), __byte_perm(m[5], m[7], 0x0040), 0x5410);
+  return even + odd * 16;
+}
+
+// A CTA: the tokens of one sample and kv-head that fall into one tile.  Tiles of a sample: from the one that its first row lies in.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) packed_write_kernel(PackedView c, RowSource src, int I, long long rows,
+__global__ void __launch_bounds__(kThreads) packed_write_kernel(PackedView c, RowSource src, int I, int tiles_per_sample,
                                                                 const int32_t* start, const int32_t* counts) {
-  constexpr int G = D / kPackedGroup, kPerRow = D / 8;
-  pdl_wait();
-  const long long row = ((long long)blockIdx.x * kThreads + threadIdx.x) / kPerRow;
-  const int part = threadIdx.x % kPerRow, group = part / 4, quad = part % 4;
-  const bool valid = row < rows;
-  const long long token_row = valid ? row / c.Hkv : 0;
-  const int head = valid ? (int)(row % c.Hkv) : 0, smp = (int)(token_row / I), token = (int)(token_row % I);
-  bool kept = valid && (counts == nullptr || token < counts[smp]);
-  const long long at = (long long)(start != nullptr ? start[smp] : 0) + token;
-  if (kept && (at < 0 || at >= c.capacity)) {
-    kept = false;
-    if (part == 0) atomicExch(c.status, kErrCapacity);
-  }
-  if (!__any_sync(0xffffffffu, kept)) return;
-  float x[2][8] = {};
-  if (kept) {
-    load8(static_cast<const T*>(src.k) + smp * src.k_sample + token * src.k_token + head * src.k_head + part * 8, x[0]);
-    load8(static_cast<const T*>(src.v) + smp * src.v_sample + token * src.v_token + head * src.v_head + part * 8, x[1]);
-  }
-  const __half sk = group_scale(x[0], quad), sv = group_scale(x[1], quad);
-  const float fk = __half2float(sk), fv = __half2float(sv);
-  // a NaN scale: the codes do not matter, but are the same for the same rows
-  const uint32_t wk = fk == fk ? quantise8(x[0], fk) : 0x88888888u, wv = fv == fv ? quantise8(x[1], fv) : 0x88888888u;
-  if (!kept) return;
   using L = PackedLayout<D>;
-  uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + (size_t)at / kPackedTile) * L::kBytes;
-  const int in = (int)(at % kPackedTile);
-  uint8_t* kc = tile + in * (D / 2);
-  *reinterpret_cast<uint32_t*>(kc + quad * 4 * G + group * 4) = wk;
-  *reinterpret_cast<uint16_t*>(tile + L::value_codes(in, group, 2 * quad)) = (uint16_t)wv;
-  *reinterpret_cast<uint16_t*>(tile + L::value_codes(in, group, 2 * quad + 1)) = (uint16_t)(wv >> 16);
-  if (quad == 0) {
-    *reinterpret_cast<__half*>(tile + L::kKeyScales + (in * G + group) * 2) = sk;
-    *reinterpret_cast<__half*>(tile + L::value_scale(in, group)) = sv;
+  constexpr int G = L::G, kPerRow = D / 8, kSteps = kPackedTile * kPerRow / kThreads, kVec = sizeof(T) / 2;
+  __shared__ __align__(16) uint8_t image[L::kBytes];
+  pdl_wait();
+  const int head = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, tile_of_sample = rest % tiles_per_sample, smp = rest / tiles_per_sample;
+  const int begin = start != nullptr ? start[smp] : 0, count = counts != nullptr ? min(counts[smp], I) : I;
+  const long long row0 = ((long long)(begin >> 5) + tile_of_sample) * kPackedTile;   // of the tile
+  const long long lo = max((long long)begin, row0), hi = min((long long)begin + count, row0 + kPackedTile);   // rows to store, [lo, hi)
+  if (hi <= lo) return;
+  if (lo < 0 || hi > c.capacity) {
+    if (threadIdx.x == 0) atomicExch(c.status, kErrCapacity);
+  }
+  if (hi <= 0 || lo >= c.capacity) return;
+  const int first = (int)(max(lo, 0ll) - row0), last = (int)(min(hi, (long long)c.capacity) - row0);   // rows of the tile, [first, last)
+  const int part = threadIdx.x % kPerRow, group = part / 4, quad = part % 4;
+  const T* k = static_cast<const T*>(src.k) + smp * src.k_sample + head * src.k_head + part * 8;
+  const T* v = static_cast<const T*>(src.v) + smp * src.v_sample + head * src.v_head + part * 8;
+  uint4 raw[kSteps][2][kVec];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int row = threadIdx.x / kPerRow + i * (kThreads / kPerRow);
+    const long long token = row0 + row - begin;
+    const bool in = row >= first && row < last;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      raw[i][0][j] = in ? ld_global_16(k + token * src.k_token + 4 * j) : make_uint4(0, 0, 0, 0);
+      raw[i][1][j] = in ? ld_global_16(v + token * src.v_token + 4 * j) : make_uint4(0, 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int row = threadIdx.x / kPerRow + i * (kThreads / kPerRow);
+    float x[8];
+    unpack8<T>(raw[i][0], x);
+    __half s = group_scale(x, quad);
+    *reinterpret_cast<uint32_t*>(image + row * (D / 2) + quad * 4 * G + group * 4) = quantise8<T>(x, __half2float(s));
+    if (quad == 0) *reinterpret_cast<__half*>(image + L::kKeyScales + (row * G + group) * 2) = s;
+    unpack8<T>(raw[i][1], x);
+    s = group_scale(x, quad);
+    const uint32_t w = quantise8<T>(x, __half2float(s));
+    *reinterpret_cast<uint16_t*>(image + L::value_codes(row, group, 2 * quad)) = (uint16_t)w;
+    *reinterpret_cast<uint16_t*>(image + L::value_codes(row, group, 2 * quad + 1)) = (uint16_t)(w >> 16);
+    if (quad == 0) *reinterpret_cast<__half*>(image + L::value_scale(row, group)) = s;
+  }
+  __syncthreads();
+  uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + (size_t)(row0 / kPackedTile)) * L::kBytes;
+  if (first == 0 && last == kPackedTile) {
+    for (int i = threadIdx.x; i < L::kBytes / 16; i += kThreads)
+      reinterpret_cast<uint4*>(tile)[i] = reinterpret_cast<const uint4*>(image)[i];
+    return;
+  }
+  // some rows only, the others are left as they were: rows of key codes and scales lie together, those of values do not
+  for (int i = threadIdx.x; i < kPackedTile * D / 32; i += kThreads)
+    if (i / (D / 32) >= first && i / (D / 32) < last) reinterpret_cast<uint4*>(tile)[i] = reinterpret_cast<const uint4*>(image)[i];
+  if (threadIdx.x < kPackedTile * G) {
+    const int row = threadIdx.x / G, g = threadIdx.x % G, ks = L::kKeyScales + threadIdx.x * 2, vs = L::value_scale(row, g);
+    if (row >= first && row < last) {
+      *reinterpret_cast<uint16_t*>(tile + ks) = *reinterpret_cast<const uint16_t*>(image + ks);
+      *reinterpret_cast<uint16_t*>(tile + vs) = *reinterpret_cast<const uint16_t*>(image + vs);
+    }
+  }
+  for (int i = threadIdx.x; i < kPackedTile * 8 * G; i += kThreads) {
+    const int row = i % 2 * 4 + i / 2 / G % 4 + i / (64 * G) * 8;   // (value_codes the other way round)
+    if (row >= first && row < last)
+      reinterpret_cast<uint16_t*>(tile + L::kValueCodes)[i] = reinterpret_cast<const uint16_t*>(image + L::kValueCodes)[i];
   }
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T* p, uint32_t w, float s);
-template <>
-__device__ __forceinline__ void store8<float>(float* p, uint32_t w, float s) {
+__device__ __forceinline__ void store8(T* p, uint32_t w, float s) {
   float f[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) f[i] = (float)((int)((w >> (4 * i)) & 15u) - 8) * s;
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
-}
-template <>
-__device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16* p, uint32_t w, float s) {
-  uint32_t o[4];
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *reinterpret_cast<float4*>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+  } else {
+    uint32_t o[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 pair = __floats2bfloat162_rn((float)((int)((w >> (8 * i)) & 15u) - 8) * s,
-                                                      (float)((int)((w >> (8 * i + 4)) & 15u) - 8) * s);
-    o[i] = *reinterpret_cast<const uint32_t*>(&pair);
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 pair = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      o[i] = *reinterpret_cast<const uint32_t*>(&pair);
+    }
+    st_global_16(p, make_uint4(o[0], o[1], o[2], o[3]));
   }
-  st_global_16(p, make_uint4(o[0], o[1], o[2], o[3]));
 }
 
-// One thread: eight elements of a key row and of the value row beside it.  Row index: ((sample * count + row) * Hkv + head).
+// A CTA: the rows of one sample and kv-head that one tile has of those asked for.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) packed_read_kernel(PackedView c, int row0, int count, long long rows, const int32_t* lens,
+__global__ void __launch_bounds__(kThreads) packed_read_kernel(PackedView c, int row0, int count, int tiles_per_sample, const int32_t* lens,
                                                                T* k_out, T* v_out) {
-  constexpr int G = D / kPackedGroup, kPerRow = D / 8;
+  using L = PackedLayout<D>;
+  constexpr int G = L::G, kPerRow = D / 8;
+  __shared__ __align__(16) uint8_t image[L::kBytes];
   pdl_wait();
-  const long long row = ((long long)blockIdx.x * kThreads + threadIdx.x) / kPerRow;
-  if (row >= rows) return;
-  const int part = threadIdx.x % kPerRow, group = part / 4, quad = part % 4;
-  const long long token_row = row / c.Hkv;
-  const int head = (int)(row % c.Hkv), smp = (int)(token_row / count), at = row0 + (int)(token_row % count);
-  uint32_t wk = 0x88888888u, wv = 0x88888888u;
-  float fk = 0.f, fv = 0.f;
-  if (lens == nullptr || at < lens[smp]) {
-    using L = PackedLayout<D>;
-    const uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + at / kPackedTile) * L::kBytes;
-    const int in = at % kPackedTile;
-    wk = *reinterpret_cast<const uint32_t*>(tile + in * (D / 2) + quad * 4 * G + group * 4);
-    wv = *reinterpret_cast<const uint16_t*>(tile + L::value_codes(in, group, 2 * quad)) |
-         ((uint32_t)*reinterpret_cast<const uint16_t*>(tile + L::value_codes(in, group, 2 * quad + 1)) << 16);
-    fk = __half2float(*reinterpret_cast<const __half*>(tile + L::kKeyScales + (in * G + group) * 2));
-    fv = __half2float(*reinterpret_cast<const __half*>(tile + L::value_scale(in, group)));
+  const int head = blockIdx.x % c.Hkv, rest = blockIdx.x / c.Hkv, smp = rest / tiles_per_sample;
+  const int t = row0 / kPackedTile + rest % tiles_per_sample, base = t * kPackedTile;
+  const int first = max(row0 - base, 0), last = min(row0 + count - base, kPackedTile);   // rows of the tile, [first, last)
+  const int len = lens != nullptr ? min(max(lens[smp] - base, 0), kPackedTile) : kPackedTile;
+  const uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + t) * L::kBytes;
+  for (int i = threadIdx.x; i < L::kBytes / 16; i += kThreads) {
+    // pieces of key codes are of one row, those of value codes of eight
+    const int piece = i * 16 - L::kValueCodes, row = piece >= 0 ? piece / (8 * D / 2) * 8 : i / (D / 32);
+    const bool wanted = piece >= 0 ? row + 8 > first && row < last : i * 16 >= L::kCodes || (row >= first && row < last);
+    if (wanted) reinterpret_cast<uint4*>(image)[i] = ld_global_16(tile + i * 16);
   }
-  store8(k_out + row * D + part * 8, wk, fk);
-  store8(v_out + row * D + part * 8, wv, fv);
+  __syncthreads();
+  const int part = threadIdx.x % kPerRow, group = part / 4, quad = part % 4;
+#pragma unroll
+  for (int i = 0; i < kPackedTile * kPerRow / kThreads; ++i) {
+    const int row = threadIdx.x / kPerRow + i * (kThreads / kPerRow);
+    if (row < first || row >= last) continue;
+    uint32_t wk = 0x88888888u, wv = 0x88888888u;
+    float fk = 0.f, fv = 0.f;
+    if (row < len) {
+      wk = *reinterpret_cast<const uint32_t*>(image + row * (D / 2) + quad * 4 * G + group * 4);
+      wv = *reinterpret_cast<const uint16_t*>(image + L::value_codes(row, group, 2 * quad)) |
+           ((uint32_t)*reinterpret_cast<const uint16_t*>(image + L::value_codes(row, group, 2 * quad + 1)) << 16);
+      fk = __half2float(*reinterpret_cast<const __half*>(image + L::kKeyScales + (row * G + group) * 2));
+      fv = __half2float(*reinterpret_cast<const __half*>(image + L::value_scale(row, group)));
+    }
+    const size_t out = (((size_t)smp * count + (base + row - row0)) * c.Hkv + head) * D + part * 8;
+    store8(k_out + out, wk, fk);
+    store8(v_out + out, wv, fv);
+  }
 }
 
 template <typename T, int D>
 cudaError_t write_t(const PackedView& c, const RowSource& src, int I, const int32_t* start, const int32_t* counts, cudaStream_t st) {
-  const long long rows = (long long)c.nsamples * I * c.Hkv, blocks = (rows * (D / 8) + kThreads - 1) / kThreads;
+  const int tiles = start == nullptr ? (I + kPackedTile - 1) / kPackedTile : (I + 2 * kPackedTile - 2) / kPackedTile;   // that I rows may touch
+  const long long blocks = (long long)c.nsamples * tiles * c.Hkv;
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  const cudaError_t err = launch_dependent(packed_write_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, src, I, rows,
-                                           start, counts);
+  const cudaError_t err = launch_dependent(packed_write_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, src, I, tiles, start,
+                                           counts);
   count_launch();
   return err != cudaSuccess ? err : cudaGetLastError();
 }
 
 template <typename T, int D>
 cudaError_t read_t(const PackedView& c, int row0, int count, const int32_t* lens, void* k_out, void* v_out, cudaStream_t st) {
-  const long long rows = (long long)c.nsamples * count * c.Hkv, blocks = (rows * (D / 8) + kThreads - 1) / kThreads;
+  const int tiles = (row0 + count - 1) / kPackedTile - row0 / kPackedTile + 1;
+  const long long blocks = (long long)c.nsamples * tiles * c.Hkv;
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  const cudaError_t err = launch_dependent(packed_read_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, row0, count, rows,
+  const cudaError_t err = launch_dependent(packed_read_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, row0, count, tiles,
                                            lens, static_cast<T*>(k_out), static_cast<T*>(v_out));
   count_launch();
   return err != cudaSuccess ? err : cudaGetLastError();
