@@ -52,6 +52,18 @@ struct PackedLayout {
   }
 };
 
+// x / d for 0 <= x < 2^31, 1 <= d < 2^31: with 2^(s - 1) < d <= 2^s and m = floor(2^32 (2^s - d) / d) + 1 (the round-up method of Granlund and
+// Montgomery, 1994), x / d = (mulhi(x, m) + x) >> s, which fits 32 bits for such x.
+struct FastDiv {
+  uint32_t d, m, s;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t by) : d(by), m(0), s(0) {
+    while ((1ull << s) < by) ++s;
+    m = (uint32_t)(((((1ull << s) - by) << 32) / by) + 1);
+  }
+  __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi((uint32_t)x, m) + (uint32_t)x) >> s); }
+};
+
 // Rows to quantise: element (sample, token, head) of k starts at k + sample * sample_stride + token * token_stride + head * head_stride.
 struct RowSource {
   const void *k, *v;

@@ -118,18 +118,6 @@ __device__ __forceinline__ uint32_t codes(uint32_t w) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// x / d for 0 <= x < 2^31, 1 <= d < 2^31: with 2^(s - 1) < d <= 2^s and m = floor(2^32 (2^s - d) / d) + 1 (the round-up method of Granlund and
-// Montgomery, 1994), x / d = (mulhi(x, m) + x) >> s, which fits 32 bits for such x.
-struct FastDiv {
-  uint32_t d, m, s;
-  FastDiv() = default;
-  explicit FastDiv(uint32_t by) : d(by), m(0), s(0) {
-    while ((1ull << s) < by) ++s;
-    m = (uint32_t)(((((1ull << s) - by) << 32) / by) + 1);
-  }
-  __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi((uint32_t)x, m) + (uint32_t)x) >> s); }
-};
-
 struct AttendArgs {
   PackedView c;
   const void* q;

@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes as C
 from dataclasses import dataclass
 
-from .binding import BM_BF16, BM_F32, _check, _sz, _vp, bm_packed_config_t, lib
+from .binding import BM_BF16, BM_F32, _check, _sz, _vp, bm_packed_config_t, fastcall, lib
 
 
 @dataclass
@@ -82,11 +82,17 @@ class PackedCache:
         _check(lib().bm_packed_create(C.byref(c), self.arena.data_ptr(), self.arena.numel(), self._stream(stream), C.byref(h)),
                "bm_packed_create")
         self.h = h
+        self._fast = fastcall()   # calls of plain tensors on the current stream go through csrc/fastcall.cpp
+        handle = (h.value, cfg.dtype == "bf16", cfg.device, cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim)
+        address = lambda fn: C.cast(fn, _vp).value
+        self._fast_write = (address(lib().bm_packed_write), *handle)
+        self._fast_read = (address(lib().bm_packed_read), *handle)
+        self._fast_attend = (address(lib().bm_packed_attend), *handle)
 
     def close(self):
         if getattr(self, "h", None) is not None and self.h:
             lib().bm_packed_destroy(self.h)
-            self.h = None
+            self.h = self._fast = None
 
     def __del__(self):
         try:
@@ -131,6 +137,12 @@ class PackedCache:
     # -- the calls --------------------------------------------------------------------------------------
     def write(self, k, v, start=None, counts=None, layer: int = 0, sample0: int = 0, stream=None):
         """k, v (ns, I, Hkv, d): token i of sample s goes to row start[s] + i (start None: row i), the first counts[s] only."""
+        if stream is None and self._fast is not None:
+            rc = self._fast.packed_write(*self._fast_write, k, v, start, counts, layer, sample0)
+            if rc is not None:
+                if rc:
+                    _check(rc, "bm_packed_write")
+                return
         assert v.shape == k.shape, "k and v must have one shape"
         ns, I = k.shape[0], k.shape[1]
         strides = (C.c_int64 * 4)(*self._check_rows(k, self.cfg.n_kv_heads), *self._check_rows(v, self.cfg.n_kv_heads))
@@ -149,6 +161,12 @@ class PackedCache:
              stream=None):
         """(k, v), each (ns, rows, Hkv, d): what rows row0 .. stand for, zeros at and past lens[s]."""
         ns = self.cfg.batch - sample0 if nsamples is None else nsamples
+        if stream is None and out is None and self._fast is not None:
+            got = self._fast.packed_read(*self._fast_read, row0, rows, layer, sample0, ns, lens)
+            if got is not None:
+                if type(got) is int:
+                    _check(got, "bm_packed_read")
+                return got
         shape = (ns, rows, self.cfg.n_kv_heads, self.cfg.head_dim)
         if out is None:
             with self._on(stream):
@@ -164,6 +182,13 @@ class PackedCache:
 
     def attend(self, q, lens, first=None, max_len: int = 0, out=None, workspace=None, layer: int = 0, sample0: int = 0, stream=None):
         """q (ns, I, Hq, d) over rows first[s] .. of caches of lens[s] rows, causal among the I; returns out (ns, I, Hq, d)."""
+        if stream is None and self._fast is not None:
+            got = self._fast.packed_attend(*self._fast_attend, q, lens, first, out, self.workspace if workspace is None else workspace,
+                                           max_len, layer, sample0)
+            if got is not None:
+                if type(got) is int:
+                    _check(got, "bm_packed_attend")
+                return got
         strides = (C.c_int64 * 2)(*self._check_rows(q, self.cfg.n_q_heads))
         ns, I = q.shape[0], q.shape[1]
         if out is None:
