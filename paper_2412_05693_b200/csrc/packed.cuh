@@ -88,6 +88,10 @@ struct PackedAttend {
 };
 // Bytes for calls of up to this many samples, kv-heads and queries.
 size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles);
+// (packed_block.cu) the same for blocks of queries, bf16
+size_t packed_block_workspace(int batch, int Hkv);
+cudaError_t launch_packed_block(int d, const PackedView& c, const PackedAttend& a, cudaStream_t st);
+bool packed_block_pays(int d, const PackedView& c, int I, int max_len);
 cudaError_t launch_packed_attend(int dtype, int d, const PackedView& c, const PackedAttend& a, cudaStream_t st);
 
 }  // namespace bm

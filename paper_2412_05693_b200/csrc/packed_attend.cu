@@ -874,10 +874,11 @@ size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, in
     const int64_t all = (int64_t)batch * Hkv * ((cols + 8 * nt - 1) / (8 * nt)) * tiles;
     most = std::max(most, (size_t)std::min(all, (int64_t)kMostSms * (nt == 1 ? 12 : 8)) * 2 * std::min<int64_t>(8 * nt, cols) * (d + 4) * sizeof(float));
   }
-  return before_bytes(batch) + most;
+  return std::max(before_bytes(batch) + most, packed_block_workspace(batch, Hkv));
 }
 
 cudaError_t launch_packed_attend(int dtype, int d, const PackedView& c, const PackedAttend& p, cudaStream_t st) {
+  if (dtype == 1 && packed_block_pays(d, c, p.I, p.max_len)) return launch_packed_block(d, c, p, st);
   AttendArgs a;
   a.c = c;
   a.q = p.q; a.q_sample = p.q_sample; a.q_token = p.q_token;

@@ -1,0 +1,537 @@
+// Attention of blocks of queries over a packed cache (packed.cuh) on the 5th-generation tensor cores: what packed_attend.cu computes, for
+// calls whose query rows, I * g of a cache, fill tiles of 128.
+//
+// A CTA has two tiles of 128 query rows of one cache, A and B, and 128 keys at a time.  Four warps turn the packed rows into fp16 tiles in
+// shared memory (K as code * s, V likewise: 15 bits rounded to 11), one issues S = Q K^T of both, one each O += P V of A and of B, and
+// four softmax warps per tile have a thread for every query row, which also brought its row of Q.  Tensor memory: O_A | O_B | P_A | P_B | S
+// (one of 128 columns that the tiles use in turn at d = 128, one each at d = 64).  A group reads its row's 128 logits into registers at once
+// and gives S back; P has columns of its own, so that the next Q K^T and the P V before run under the exponentials.
+//
+// fp16 has 40 binades: keys and values are taken times a power of two per cache (packed_scales_kernel finds the largest scale), queries per
+// row, and what remains below fp16's smallest is 2^-38 of the largest.  Elements of every eight are kept in the order 0 4 1 5 2 6 3 7, in
+// which two masked codes are neighbours, in Q as in K; outputs are put in order on their way out.
+//
+// A scale that is not finite: keys give NaN logits.  A weight of 0 times a NaN value would be NaN for queries that do not see the row, so such
+// values are 0 in the tile, and the first such row of each group is kept: queries see a prefix of the rows, those that see it are NaN there.
+//
+// What bounds it: the softmax warps (exponentials 2048 cycles per pair of tiles, the tensor pipe as many) and, beside them on the same
+// schedulers, the unpacking (13 instructions for 8 elements, 430 per thread and 128 keys).
+#include <algorithm>
+#include <cmath>
+
+#include "packed.cuh"
+#include "tc_common.cuh"
+
+namespace bm {
+using namespace tc;
+namespace {
+
+constexpr int kRows = 128, kKeys = 128, kThreads = 512;
+constexpr int kScaleParts = 16;         // CTAs that look at a cache's scales
+constexpr float kRescale = 8.f;         // the maximum follows when logits pass it by this much (log2): weights stay below 2^8
+
+struct BlockArgs16 {
+  PackedView c;
+  const __nv_bfloat16* q;
+  int64_t q_sample, q_token;
+  int32_t I;
+  const int32_t* lens;
+  const int32_t* first;
+  __nv_bfloat16* out;
+  float mul;              // scale * log2(e)
+  int32_t pairs;          // of row tiles, per cache
+  FastDiv by_g, by_pairs, by_heads;
+  uint32_t* largest;      // workspace: [units][kScaleParts][2] largest finite magnitudes of the key scales, the value scales (fp16 bits)
+};
+
+struct Seen {
+  int len, lo;            // rows [lo, len) are seen by some query
+};
+__device__ __forceinline__ Seen seen_rows(const BlockArgs16& a, int smp) {
+  Seen s;
+  s.len = min(max(a.lens[smp], 0), a.c.capacity);
+  s.lo = a.first != nullptr ? max(a.first[smp], 0) : 0;
+  return s;
+}
+
+// The largest scales of a cache, in kScaleParts parts.
+template <int D>
+__global__ void __launch_bounds__(256) packed_scales_kernel(BlockArgs16 a) {
+  using L = PackedLayout<D>;
+  constexpr int kPieces = 2 * L::kScales / 16, kTilesPerStep = 256 / kPieces;   // 16-byte pieces of a tile's scales
+  __shared__ uint32_t warp_max[8][2];
+  pdl_wait();
+  pdl_release();
+  const int unit = blockIdx.x / kScaleParts, part = blockIdx.x % kScaleParts, smp = a.by_heads(unit);
+  const Seen seen = seen_rows(a, smp);
+  const int t0 = seen.lo / kPackedTile, t1 = seen.len > seen.lo ? (seen.len + kPackedTile - 1) / kPackedTile : t0;
+  const uint8_t* base = a.c.data + (size_t)unit * a.c.tiles * L::kBytes;
+  const int piece = threadIdx.x % kPieces;
+  uint32_t most = 0;
+#pragma unroll 4
+  for (int t = t0 + part * kTilesPerStep + threadIdx.x / kPieces; t < t1; t += kScaleParts * kTilesPerStep) {
+    const uint4 v = ld_global_16(base + (size_t)t * L::kBytes + L::kKeyScales + piece * 16);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;
+      most = max(most, max(lo < 0x7c00u ? lo : 0u, hi < 0x7c00u ? hi : 0u));
+    }
+  }
+  const bool value = piece >= kPieces / 2;
+  const uint32_t k = __reduce_max_sync(0xffffffffu, value ? 0u : most), v = __reduce_max_sync(0xffffffffu, value ? most : 0u);
+  if (threadIdx.x % 32 == 0) {
+    warp_max[threadIdx.x / 32][0] = k;
+    warp_max[threadIdx.x / 32][1] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    uint32_t m = 0;
+    for (int i = 0; i < 8; ++i) m = max(m, warp_max[i][threadIdx.x]);
+    a.largest[(size_t)blockIdx.x * 2 + threadIdx.x] = m;
+  }
+}
+
+template <int D>
+struct BlockSmem {
+  static constexpr int kTile = kRows * D * 2;     // 128 rows of D fp16 numbers, in pieces of 64 elements: [piece][row][128 bytes, swizzled]
+  static constexpr int kQ = 0, kK = 2 * kTile, kV = 4 * kTile, kBars = 6 * kTile, kTotal = kBars + 512 + 1024;
+};
+
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// eight codes of a word times a scale (a pair), in the order 0 4 1 5 2 6 3 7
+__device__ __forceinline__ uint4 unpack_scaled(uint32_t w, uint32_t s2) {
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t u = ((i < 2 ? w : w >> 8) & (i % 2 ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;   // 1024 + u, 1024 + 16 u
+    const __half2 h = *reinterpret_cast<const __half2*>(&u);
+    const __half2 c = i % 2 ? __hfma2(h, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hsub2(h, __float2half2_rn(1032.f));
+    x[i] = hmul2(*reinterpret_cast<const uint32_t*>(&c), s2);
+  }
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ bool not_finite(uint32_t s) { return (s & 0x7c00u) == 0x7c00u; }   // of an fp16 number in the low half
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a) {
+  using S = BlockSmem<D>;
+  using L = PackedLayout<D>;
+  constexpr int G = L::G, kQkWarp = 8, kPvWarp = 9 /* A; 10: B */, kUnpackWarp = 12;
+  constexpr int NSB = D == 128 ? 1 : 2;   // logit buffers
+  constexpr int B_Q = 0, B_KFULL = 2, B_KFREE = 4, B_VFULL = 6, B_VFREE = 8, B_SFULL = 10, B_SFREE = 12, B_P = 14 /* [half][group] */,
+                B_PV = 18 /* likewise */, B_COUNT = 22;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* sm = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + S::kBars);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + B_COUNT);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* nan_row = reinterpret_cast<int*>(tmem_slot + 2);   // [4]
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();   // (before tensor memory is taken: a kernel before may have CTAs that wait for it)
+  pdl_release();
+  if (tid == 0) {
+    *abort_flag = 0;
+#pragma unroll 1
+    for (int b = 0; b < B_COUNT; ++b)
+      mbar_init(&bars[b], b < B_KFREE || (b >= B_VFULL && b < B_VFREE) || (b >= B_SFREE && b < B_PV) ? 4 : b >= B_VFREE && b < B_SFULL ? 2 : 1);
+    mbar_fence_init();
+    for (int i = 0; i < 4; ++i) nan_row[i] = INT32_MAX;
+  }
+  if (warp == kQkWarp) tmem_alloc(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const uint32_t tm_o0 = tmem, tm_p0 = tmem + 2 * D, tm_s0 = tmem + 2 * D + 128;   // group x: + D x, + 64 x, + 128 x (NSB = 2)
+  auto wait = [&](int b, int n) { mbar_wait(&bars[b], (uint32_t)n & 1, abort_flag, a.c.status); };   // for the n-th completion
+
+  const int unit = a.by_pairs(blockIdx.x), pair = a.pairs - 1 - (blockIdx.x - unit * a.pairs);   // (later rows see more keys: first)
+  const int smp = a.by_heads(unit), head = unit - smp * a.c.Hkv;
+  const Seen seen = seen_rows(a, smp);
+  const int cols = a.I * a.c.g, t_first = seen.lo / kKeys;
+  // key tiles that row tile x sees: up to its last row's limit
+  auto key_tiles = [&](int x) {
+    const int row0 = (2 * pair + x) * kRows;
+    if (row0 >= cols) return 0;
+    const int limit = seen.len - (a.I - 1 - a.by_g(min(row0 + kRows, cols) - 1));
+    return limit > seen.lo ? (limit + kKeys - 1) / kKeys - t_first : 0;
+  };
+  const int n0 = key_tiles(0), n1 = key_tiles(1), T = max(n0, n1);
+  // powers of two that bring the largest key and value scale to 2^11 .. 2^12 (times 8: below 2^15)
+  int ek = 0, ev = 0;
+  {
+    const uint32_t* p = a.largest + (size_t)unit * kScaleParts * 2;
+    uint32_t mk = 0, mv = 0;
+#pragma unroll
+    for (int i = 0; i < kScaleParts; ++i) { mk = max(mk, p[2 * i]); mv = max(mv, p[2 * i + 1]); }
+    const float fk = __half2float(__ushort_as_half((unsigned short)mk)), fv = __half2float(__ushort_as_half((unsigned short)mv));
+    if (mk > 0) ek = 11 - ((int)(__float_as_uint(fk) >> 23) - 127);
+    if (mv > 0) ev = 11 - ((int)(__float_as_uint(fv) >> 23) - 127);   // -4 .. 35
+  }
+  auto pow2 = [](int e) { return __int_as_float((e + 127) << 23); };
+
+  if (warp >= kQkWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");   // 512 threads start with 128 registers each: 256 x 168 + 256 x 88
+    if (warp >= kUnpackWarp) {
+      // ------------------------------------------------------------------ packed rows -> fp16 tiles
+      const int d = tid - kUnpackWarp * 32;
+      const uint8_t* base = a.c.data + (size_t)unit * a.c.tiles * L::kBytes;
+      const float fk = pow2(ek), fv = pow2(ev);
+      uint4 kc[D / 32], vc[2][2];   // this thread's codes: of key row d; of two pairs of value rows, 8 elements of each group
+      uint32_t ks[G / 2], vs[2][G];
+      // value task i: rows c and c + 4 of the tile's 8-row block (d + 128 i) / 16, the elements 8 rp .. + 7 of each group
+      auto load_keys = [&](int j) {
+        const int row = (t_first + j) * kKeys + d;
+        const bool in = row >= seen.lo && row < seen.len;
+        const uint8_t* tile = base + (size_t)(row / kPackedTile) * L::kBytes;
+        const int at = row % kPackedTile;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) kc[i] = in ? ld_global_16(tile + at * (D / 2) + i * 16) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) ks[i] = in ? *reinterpret_cast<const uint32_t*>(tile + L::kKeyScales + at * G * 2 + i * 4) : 0u;
+      };
+      auto load_values = [&](int j) {
+        const int row0 = (t_first + j) * kKeys;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int task = d + 128 * i, block = task / 16, rp = task / 4 % 4, c = task % 4, row = row0 + block * 8 + c;
+          const bool lo_in = row >= seen.lo && row < seen.len, hi_in = row + 4 >= seen.lo && row + 4 < seen.len;
+          const uint8_t* tile = base + (size_t)(row / kPackedTile) * L::kBytes;
+          const int at = row % kPackedTile;
+          const uint32_t keep = (lo_in ? 0x0000ffffu : 0u) | (hi_in ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int g4 = 0; g4 < G; ++g4) vs[i][g4] = 0u;
+          vc[i][0] = vc[i][1] = make_uint4(0, 0, 0, 0);
+          if (keep != 0) {
+            if constexpr (G == 4) {
+              vc[i][0] = ld_global_16(tile + L::value_codes(at, 0, 2 * rp));
+              vc[i][1] = ld_global_16(tile + L::value_codes(at, 0, 2 * rp + 1));
+              const uint4 s = ld_global_16(tile + L::value_scale(at, 0));
+              vs[i][0] = s.x; vs[i][1] = s.y; vs[i][G - 2] = s.z; vs[i][G - 1] = s.w;
+            } else {
+              const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_codes(at, 0, 2 * rp));
+              const uint2 y = *reinterpret_cast<const uint2*>(tile + L::value_codes(at, 0, 2 * rp + 1));
+              vc[i][0] = make_uint4(x.x, x.y, 0, 0);
+              vc[i][1] = make_uint4(y.x, y.y, 0, 0);
+              const uint2 s = *reinterpret_cast<const uint2*>(tile + L::value_scale(at, 0));
+              vs[i][0] = s.x; vs[i][1] = s.y;
+            }
+#pragma unroll
+            for (int g4 = 0; g4 < G; ++g4) vs[i][g4] &= keep;
+          }
+        }
+      };
+      if (T > 0) {
+        load_keys(0);
+        load_values(0);
+      }
+#pragma unroll 1
+      for (int j = 0; j < T; ++j) {
+        const int s = j & 1;
+        if (j >= 2) wait(B_KFREE + s, j / 2 - 1);
+        unsigned char* k = sm + S::kK + s * S::kTile;
+#pragma unroll
+        for (int g4 = 0; g4 < G; ++g4) {
+          const float f = __half2float(__ushort_as_half((unsigned short)(ks[g4 / 2] >> (16 * (g4 % 2))))) * fk;
+          const uint32_t s2 = half2_bits(f, f);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {   // the word (g4, c): word c G + g4 of the row
+            const int at = c * G + g4;
+            const uint4 four = kc[at / 4];
+            const uint32_t w = at % 4 == 0 ? four.x : at % 4 == 1 ? four.y : at % 4 == 2 ? four.z : four.w;
+            *reinterpret_cast<uint4*>(k + (4 * g4 + c) / 8 * 16384 + sw128_offset(d, (4 * g4 + c) % 8)) = unpack_scaled(w, s2);
+          }
+        }
+        if (j + 1 < T) load_keys(j + 1);   // (on its way while the values are unpacked, and theirs during the next keys)
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_KFULL + s]);
+        if (j >= 2) wait(B_VFREE + s, j / 2 - 1);
+        unsigned char* v = sm + S::kV + s * S::kTile;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int task = d + 128 * i, block = task / 16, rp = task / 4 % 4, c = task % 4;
+#pragma unroll
+          for (int g4 = 0; g4 < G; ++g4) {
+            const uint32_t x = g4 == 0 ? vc[i][0].x : g4 == 1 ? vc[i][0].y : g4 == 2 ? vc[i][0].z : vc[i][0].w;
+            const uint32_t y = g4 == 0 ? vc[i][1].x : g4 == 1 ? vc[i][1].y : g4 == 2 ? vc[i][1].z : vc[i][1].w;
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+              const uint32_t bits = vs[i][g4] >> (16 * hi) & 0xffffu;
+              float f = __half2float(__ushort_as_half((unsigned short)bits)) * fv;
+              if (not_finite(bits)) {
+                atomicMin(&nan_row[g4], (t_first + j) * kKeys + block * 8 + c + 4 * hi);
+                __threadfence_block();
+                f = 0.f;
+              }
+              const int piece = 4 * g4 + rp;
+              *reinterpret_cast<uint4*>(v + piece / 8 * 16384 + sw128_offset(block * 8 + c + 4 * hi, piece % 8)) =
+                  unpack_scaled(__byte_perm(x, y, hi ? 0x7632 : 0x5410), half2_bits(f, f));
+            }
+          }
+        }
+        if (j + 1 < T) load_values(j + 1);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_VFULL + s]);
+      }
+    } else if (lane == 0) {
+      const uint64_t dk_hi = smem_desc(0, 16, 1024) & 0xffffffff00000000ull;      // K-major operands (Q, K)
+      const uint32_t dk_lo = (uint32_t)(smem_desc(0, 16, 1024) & 0xffffffffull);
+      const uint64_t dv_hi = smem_desc(0, 16384, 1024) & 0xffffffff00000000ull;   // MN-major operand (V)
+      const uint32_t dv_lo = (uint32_t)(smem_desc(0, 16384, 1024) & 0xffffffffull);
+      constexpr uint32_t kBf16 = 1u << 7 | 1u << 10;                               // instr_desc's input formats: cleared, fp16
+      if (warp == kQkWarp) {
+        // ---------------------------------------------------------------- S = Q K^T of both tiles, in turn
+        const uint32_t idesc = instr_desc(kRows, kKeys, 0, 0) & ~kBf16;
+        const uint32_t q_lo = dk_lo + (smem_u32(sm + S::kQ) >> 4), k_base = dk_lo + (smem_u32(sm + S::kK) >> 4);
+        int sc0 = 0, sc1 = 0, last = -1;
+#pragma unroll 1
+        for (int j = 0; j < T; ++j) {
+          wait(B_KFULL + (j & 1), j / 2);
+          const uint32_t k_lo = k_base + (uint32_t)(j & 1) * (S::kTile >> 4);
+#pragma unroll 1
+          for (int x = 0; x < 2; ++x) {
+            if (j >= (x ? n1 : n0)) continue;
+            if (j == 0) wait(B_Q + x, 0);
+            const int before = NSB == 2 ? x : last, n = before == 0 ? sc0 : sc1;   // the logits that the buffer holds have been read
+            if (before >= 0 && n > 0) wait(B_SFREE + before, n - 1);
+            last = x;
+            if (x == 0) ++sc0; else ++sc1;
+            tc_fence_after();
+            const uint32_t q = q_lo + x * (S::kTile >> 4);
+#pragma unroll
+            for (int step = 0; step < D / 16; ++step) {
+              const uint32_t off = (step >> 2) * 1024 + (step & 3) * 2;   // (piece * 16384 + step * 32) / 16
+              mma_ss(tm_s0 + (NSB == 2 ? 128 * x : 0), dk_hi | (q + off), dk_hi | (k_lo + off), idesc, step > 0 ? 1u : 0u);
+            }
+            mma_commit(&bars[B_SFULL + x]);
+          }
+          mma_commit(&bars[B_KFREE + (j & 1)]);
+        }
+      } else if (warp == kPvWarp || warp == kPvWarp + 1) {
+        // ---------------------------------------------------------------- O += P V of tile x, 64 keys at a time
+        const int x = warp - kPvWarp, n = x ? n1 : n0;
+        const uint32_t idesc = instr_desc(kRows, D, 0, 1) & ~kBf16;   // V is MN-major: d contiguous, keys along K
+        const uint32_t v_base = dv_lo + (smem_u32(sm + S::kV) >> 4);
+        const uint32_t tm_o = tm_o0 + D * x, tm_p = tm_p0 + 64 * x;
+#pragma unroll 1
+        for (int j = 0; j < T; ++j) {
+          wait(B_VFULL + (j & 1), j / 2);
+          if (j >= n) { mbar_arrive(&bars[B_VFREE + (j & 1)]); continue; }
+          const uint32_t v_lo = v_base + (uint32_t)(j & 1) * (S::kTile >> 4);
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            wait(B_P + 2 * h + x, j);
+            tc_fence_after();
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              mma_ts(tm_o, tm_p + (4 * h + q) * 8, dv_hi | (v_lo + (4 * h + q) * 128), idesc, j > 0 || h > 0 || q > 0 ? 1u : 0u);
+            mma_commit(&bars[B_PV + 2 * h + x]);
+          }
+          mma_commit(&bars[B_VFREE + (j & 1)]);
+        }
+      }
+    }
+  } else {
+    // -------------------------------------------------------------------- a thread per query row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    const int x = warp >> 2, quad = warp & 3, r = quad * 32 + lane, n = x ? n1 : n0;
+    const int col = (2 * pair + x) * kRows + r, query = a.by_g(min(col, cols - 1)), in_group = min(col, cols - 1) - query * a.c.g;
+    const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
+    const uint32_t tm_s = tm_s0 + (NSB == 2 ? 128 * x : 0) + lane_addr, tm_p = tm_p0 + 64 * x + lane_addr, tm_o = tm_o0 + D * x + lane_addr;
+    const int limit = seen.len - (a.I - 1 - query);   // this row sees [seen.lo, limit)
+    float row_mul = 0.f;
+    if (n > 0) {   // the row of Q, to a largest magnitude of 2^14 .. 2^15
+      const __nv_bfloat16* q = a.q + smp * a.q_sample + query * a.q_token + ((size_t)head * a.c.g + in_group) * D;
+      uint4 raw[D / 8];
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        raw[i] = ld_global_16(q + 8 * i);
+        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = max(most, max(w[e] << 16 & 0x7fff0000u, w[e] & 0x7fff0000u));
+      }
+      const int e = most > 0 && most < 0x7f800000u ? min(14 - (int)(most >> 23) + 127, 100) : 0;
+      const float up = pow2(e);
+      row_mul = fmaxf(a.mul * pow2(-e) * pow2(-ek), 0x1p-126f);
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        float f[8];
+        Elem<__nv_bfloat16>::unpack(raw[i], f);
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = half2_bits(f[k] * up, f[k + 4] * up);
+        *reinterpret_cast<uint4*>(sm + S::kQ + x * S::kTile + i / 8 * 16384 + sw128_offset(r, i % 8)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_Q + x]);
+    }
+    float m_used = -INFINITY, l = 0.f;
+#pragma unroll 1
+    for (int j = 0; j < n; ++j) {
+      wait(B_SFULL + x, j);
+      tc_fence_after();
+      const int row0 = (t_first + j) * kKeys, v0 = max(seen.lo - row0, 0), v1 = min(limit - row0, kKeys);   // visible columns [v0, v1)
+      if (!__all_sync(0xffffffffu, v0 == 0 && v1 == kKeys)) {
+        // hidden logits become -inf, in tensor memory and in a rolled loop: these tiles are few
+#pragma unroll 1
+        for (int cc = 0; cc < 8; ++cc) {
+          uint32_t raw[16];
+          tmem_ld16(tm_s + 16 * cc, raw);
+          const int b0 = min(max(v0 - 16 * cc, 0), 16), b1 = min(max(v1 - 16 * cc, 0), 16);
+          const uint32_t bits = ((1u << b1) - 1u) & ~((1u << b0) - 1u);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) raw[e] = (bits >> e) & 1 ? raw[e] : 0xff800000u;
+          tmem_st16(tm_s + 16 * cc, raw);
+        }
+        tmem_wait_st();
+      }
+      uint32_t s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(tm_s + 32 * c, s[c]);
+      tmem_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_SFREE + x]);
+      float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int e = 0; e < 32; e += 2)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) m4[c] = max3_nan(m4[c], __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
+      float mx = max3_nan(max3_nan(m4[0], m4[1], m4[2]), m4[3], -INFINITY) * row_mul;
+      if (mx == INFINITY) mx = __uint_as_float(0x7fffffffu);   // an infinite logit makes its row NaN, as NaN does
+      bool rescale = false;
+      float alpha = 1.f;
+      if (j == 0) m_used = mx;
+      else if (!(mx <= m_used + kRescale)) { alpha = exp2f(m_used - mx); m_used = mx; rescale = true; }
+      if (__any_sync(0xffffffffu, rescale)) {
+        wait(B_PV + 2 + x, j - 1);
+        tc_fence_after();
+#pragma unroll 1
+        for (int cc = 0; cc < D / 16; ++cc) {
+          uint32_t raw[16];
+          tmem_ld16(tm_o + cc * 16, raw);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) raw[e] = __float_as_uint(__uint_as_float(raw[e]) * alpha);
+          tmem_st16(tm_o + cc * 16, raw);
+        }
+        l *= alpha;
+      }
+      const float neg_m = m_used == -INFINITY ? 0.f : -m_used;   // (no row seen so far)
+      float pa0 = 0.f, pa1 = 0.f, pb0 = 0.f, pb1 = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float x0, x1;
+          fma2(x0, x1, __uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1]), row_mul, neg_m);
+          const float p0 = ex2(x0), p1 = ex2(x1);
+          if (e & 1) add2(pb0, pb1, p0, p1);
+          else add2(pa0, pa1, p0, p1);
+          pk[e] = half2_bits(p0, p1);
+        }
+        if (!(c & 1) && j > 0) wait(B_PV + c + x, j - 1);   // the columns' weights of the tile before are used up
+        tmem_st16(tm_p + 16 * c, pk);
+        if (c & 1) {                            // 64 keys may enter P V
+          tmem_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[B_P + c - 1 + x]);
+        }
+      }
+      l += (pa0 + pb0) + (pa1 + pb1);
+    }
+    // ---- O / l, out in order; a row that sees nothing is a row of zeros ---------------------------------------------------------
+    __nv_bfloat16* out = a.out + (((size_t)smp * a.I + query) * a.c.Hq + (size_t)head * a.c.g + in_group) * D;
+    const bool any = n > 0 && limit > seen.lo;
+    if (n > 0) {
+      wait(B_PV + 2 + x, n - 1);
+      tc_fence_after();
+    }
+    const float by = any ? pow2(-ev) / l : 0.f;
+#pragma unroll 1
+    for (int g4 = 0; g4 < G; ++g4) {
+      uint32_t raw[32];
+      if (n > 0) {
+        tmem_ld32(tm_o + 32 * g4, raw);
+        tmem_wait_ld();
+      }
+      const float scale = any && *const_cast<volatile int*>(&nan_row[g4]) < limit ? __uint_as_float(0x7fffffffu) : by;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = any ? __uint_as_float(raw[8 * i + (k < 4 ? 2 * k : 2 * k - 7)]) * scale : 0.f;
+        if (col < cols)
+          st_global_16(out + 32 * g4 + 8 * i, make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])));
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kQkWarp) tmem_dealloc(tmem, 512);
+}
+
+template <int D>
+cudaError_t launch_d(const PackedView& c, const PackedAttend& p, cudaStream_t st) {
+  BlockArgs16 a;
+  a.c = c;
+  a.q = static_cast<const __nv_bfloat16*>(p.q);
+  a.q_sample = p.q_sample; a.q_token = p.q_token;
+  a.I = p.I;
+  a.lens = p.lens; a.first = p.first;
+  a.out = static_cast<__nv_bfloat16*>(p.out);
+  a.mul = p.scale * 1.4426950408889634f;
+  a.largest = static_cast<uint32_t*>(p.workspace);
+  const int64_t units = (int64_t)c.nsamples * c.Hkv, cols = (int64_t)p.I * c.g;
+  a.pairs = (int)((cols + 2 * kRows - 1) / (2 * kRows));
+  a.by_g = FastDiv((uint32_t)c.g);
+  a.by_pairs = FastDiv((uint32_t)a.pairs);
+  a.by_heads = FastDiv((uint32_t)c.Hkv);
+  if (units * std::max<int64_t>(a.pairs, kScaleParts) > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  static SmemConfigured configured;
+  if (cudaError_t err = configured.ensure(packed_block_kernel<D>, BlockSmem<D>::kTotal); err != cudaSuccess) return err;
+  cudaError_t err = launch_dependent(packed_scales_kernel<D>, dim3((unsigned)(units * kScaleParts)), dim3(256), 0, st, a);
+  count_launch();
+  if (err != cudaSuccess) return err;
+  err = launch_dependent(packed_block_kernel<D>, dim3((unsigned)(units * a.pairs)), dim3(kThreads), BlockSmem<D>::kTotal, st, a);
+  count_launch();
+  return err != cudaSuccess ? err : cudaGetLastError();
+}
+
+}  // namespace
+
+// Which calls take this kernel: its time goes by rounds of one CTA per SM and 128 keys, that of the warps' kernel by tiles of 32 keys x 32
+// query rows, shared evenly, and what joining them costs.  us, this kernel / the other: 32 / 8 heads, d = 128, 16 samples of 4096 rows, 32
+// query rows of a cache 100 / 92, 64 rows 100 / 156, 128 rows 102 / 223; 4 samples, 64 rows 86 / 54, 128 rows 86 / 86, 1024 rows (4352) 103 /
+// 414; 1 sample of 4352, 256 rows 97 / 55, 1024 rows 98 / 148; of 16384, 512 rows 336 / 214; 64 samples of 1024, 64 rows 119 / 177; 32 samples
+// of 2048, 32 heads without groups, 16 rows 385 / 102, 64 rows 390 / 481; 8 heads, d = 64, 4 samples of 4352, 1024 rows 76 / 193.
+bool packed_block_pays(int d, const PackedView& c, int I, int max_len) {
+  const double cols = (double)I * c.g, units = (double)c.nsamples * c.Hkv, pairs = std::ceil(cols / (2 * kRows));
+  if (cols <= 32) return false;
+  const double here = (d == 64 ? 2.1 : 2.75) * std::ceil(units * pairs / sm_count()) * max_len / kKeys;
+  const double warps = 40 + (d == 64 ? 1.3 : 3.1) * units * std::ceil(cols / 32) * max_len / kPackedTile / (8. * sm_count());
+  return here < warps;
+}
+
+size_t packed_block_workspace(int batch, int Hkv) { return (size_t)batch * Hkv * kScaleParts * 2 * sizeof(uint32_t); }
+
+cudaError_t launch_packed_block(int d, const PackedView& c, const PackedAttend& p, cudaStream_t st) {
+  return d == 64 ? launch_d<64>(c, p, st) : launch_d<128>(c, p, st);
+}
+
+}  // namespace bm

@@ -184,6 +184,7 @@ def test_the_pairs_that_a_prefill_kept_are_packed(dtype, compaction):
 
 # ---- attend -----------------------------------------------------------------------------------------------------------------
 def check_attend(b, Hq, Hkv, d, I, capacity, lens, first, dtype, seed=0, spread=1.0, scale=0.0, split=0, cache=None):
+    blocks = dtype == "bf16" and I * (Hq // Hkv) > 64       # many query rows may go through fp16 tiles
     gen = torch.Generator().manual_seed(seed)
     k, v = rows(gen, b, capacity, Hkv, d, dtype=dtype), rows(gen, b, capacity, Hkv, d, dtype=dtype, spread=spread)
     q = rows(gen, b, I, Hq, d, dtype=dtype)
@@ -191,8 +192,8 @@ def check_attend(b, Hq, Hkv, d, I, capacity, lens, first, dtype, seed=0, spread=
     cache.write(k, v)
     out = cache.attend(q, ints(lens), first=ints(first) if first is not None else None, max_len=split)
     want, wide, slack = ref.attend(q.double().cpu(), ref.packed_values(k), ref.packed_values(v), lens, first or [0] * b,
-                                   scale or d ** -0.5, DT[dtype])
-    allowed = ref.bound(want, wide, slack, DT[dtype], capacity, float(v.double().abs().max()))
+                                   scale or d ** -0.5, DT[dtype], blocks)
+    allowed = ref.bound(want, wide, slack, DT[dtype], capacity, float(v.double().abs().max()), blocks)
     err = (out.double().cpu() - want).abs()
     assert not out.isnan().any()
     assert (err <= allowed).all(), f"worst error / allowed: {(err / allowed).max():.3f}, largest error {err.max():.3e}"
@@ -224,6 +225,43 @@ def test_several_queries_are_causal(I, Hq, Hkv, dtype):
     lens = [150, I, max(I - 2, 0), 64 + I // 2, 149]
     check_attend(5, Hq, Hkv, 64, I, 150, lens, None, dtype, seed=I)
     check_attend(5, Hq, Hkv, 128, I, 150, lens, [0, 0, 0, 64, 33], dtype, seed=I + 100)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("I,Hq,Hkv", [(65, 1, 1), (128, 2, 2), (129, 1, 1), (256, 1, 1), (257, 2, 2), (40, 8, 2), (90, 6, 2), (300, 2, 1), (23, 12, 1)])
+def test_blocks_of_queries(I, Hq, Hkv, d):
+    n = 400
+    check_attend(3, Hq, Hkv, d, I, n, [n, I, 333], None, "bf16", seed=I)
+    check_attend(4, Hq, Hkv, d, I, n, [n - 1, I + 1, max(I - 3, 1), 0], [130, 0, 0, 5], "bf16", seed=I + 1)
+
+
+@pytest.mark.parametrize("spread", [1e-6, 1e-3, 100.0, 30000.0])
+def test_blocks_of_queries_over_values_of_any_size(spread):
+    check_attend(2, 2, 1, 128, 70, 200, [200, 77], None, "bf16", spread=spread, seed=31)
+
+
+def test_blocks_over_long_caches():
+    for d in (64, 128):
+        check_attend(1, 2, 1, d, 70, 3000, [2999], [100], "bf16", seed=33)
+
+
+def test_blocks_meet_rows_that_are_not_finite():
+    b, Hq, Hkv, d, I, n = 3, 2, 2, 128, 130, 300
+    gen = torch.Generator().manual_seed(34)
+    k, v, q = (rows(gen, b, t, h, d, dtype="bf16") for t, h in ((n, Hkv), (n, Hkv), (I, Hq)))
+    v[0, 200, 0, 40] = math.nan                       # group 1, head 0: queries that see row 200
+    k[1, 250, 1, 0] = math.inf                        # head 1: queries that see row 250
+    k[2, 290:], v[2, 290:] = math.nan, math.inf       # behind sample 2's length
+    k[2, :7], v[2, :7] = -math.inf, math.nan          # before its first row
+    q[2, 5, 1, 3] = math.nan
+    cache = make(b, Hq, Hkv, d, n, "bf16", queries_max=I)
+    cache.write(k, v)
+    out = cache.attend(q, ints([300, 300, 290]), first=ints([0, 0, 7])).float().cpu()
+    bad = torch.zeros(b, I, Hq, d, dtype=torch.bool)
+    bad[0, I - 99 - 1:, 0, 32:64] = True              # query i sees rows below 300 - (129 - i): row 200 from i = 30 on
+    bad[1, I - 49 - 1:, 1] = True
+    bad[2, 5, 1] = True
+    assert torch.equal(out.isnan(), bad)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -394,9 +432,25 @@ def test_a_captured_step_replayed_as_the_caches_grow():
     assert cache.status() == 0
 
 
+def test_a_captured_block_gives_what_an_eager_one_gives():
+    gen = torch.Generator().manual_seed(35)
+    cache = make(2, 4, 2, 128, 600, "bf16", queries_max=150)
+    cache.write(rows(gen, 2, 600, 2, 128, dtype="bf16"), rows(gen, 2, 600, 2, 128, dtype="bf16"))
+    q, lens = rows(gen, 2, 150, 4, 128, dtype="bf16"), ints([600, 480])
+    want = cache.attend(q, lens)
+    out = torch.zeros_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.attend(q, lens, out=out)
+    for n in ([600, 480], [333, 600]):
+        lens.copy_(ints(n))
+        graph.replay()
+        assert torch.equal(out, want if n[0] == 600 else cache.attend(q, lens))
+
+
 def test_same_results_from_run_to_run():
     gen = torch.Generator().manual_seed(20)
-    for Hq, Hkv, I, n in ((32, 8, 1, 5000), (8, 8, 1, 700), (8, 2, 9, 300)):
+    for Hq, Hkv, I, n in ((32, 8, 1, 5000), (8, 8, 1, 700), (8, 2, 9, 300), (8, 2, 200, 500)):
         cache = make(2, Hq, Hkv, 128, n, "bf16", queries_max=I)
         cache.write(rows(gen, 2, n, Hkv, 128, dtype="bf16"), rows(gen, 2, n, Hkv, 128, dtype="bf16"))
         q, lens = rows(gen, 2, I, Hq, 128, dtype="bf16"), ints([n, n - 5])
