@@ -32,7 +32,7 @@ def packed_values(x):
 
 def attend(q, k, v, lens, first, scale, dtype, blocks=False):
     """q (b, I, Hq, d), k / v (b, n, Hkv, d) float64 -> out, and per output element the sum of p |v| and the largest relative
-    error that the sums of the logits may put on a weight.  blocks: keys and values go through fp16 (calls of many queries)."""
+    error that the sums of the logits may put on a weight.  blocks: keys and values may go through fp16 (calls of many queries)."""
     b, I, Hq, d = q.shape
     n, Hkv = k.shape[1], k.shape[2]
     out = torch.zeros(b, I, Hq, d, dtype=torch.float64)
@@ -50,10 +50,7 @@ def attend(q, k, v, lens, first, scale, dtype, blocks=False):
                 p = torch.softmax(logit, 0)
                 out[s, i, h] = p @ vv[lo:hi]
                 spread[s, i, h] = p @ vv[lo:hi].abs()
-                if blocks:
-                    # every key is off by half a step of fp16 at most, and d products are added
-                    err = (kk[lo:hi].abs() @ qq.abs()) * (2.0 ** -11 + d * 2.0 ** -23)
-                elif dtype == torch.bfloat16:
+                if dtype == torch.bfloat16:
                     # A group's sum runs over 32 products u q (u <= 15) from -8 sum q: at most 40 additions of at most 23 sum |q|,
                     # each off by a step of fp32, 2^-23; times the scale, an eighth of the group's largest |k| (1 + 2^-10).
                     size = kk[lo:hi].abs().view(hi - lo, -1, GROUP).amax(-1) / 8 * (1 + 2 ** -10)
@@ -61,6 +58,8 @@ def attend(q, k, v, lens, first, scale, dtype, blocks=False):
                     # up to four query rows of a cache are integers, each element off by half a step, 2^-15 of the row's largest
                     if I * (Hq // Hkv) <= 4:
                         err = err + kk[lo:hi].abs().sum(-1) * qq.abs().max() * 2.0 ** -14
+                    if blocks:   # every key may be off by half a step of fp16, and d products are added
+                        err = torch.maximum(err, (kk[lo:hi].abs() @ qq.abs()) * (2.0 ** -11 + d * 2.0 ** -23))
                 else:
                     # 64 products (two halves of q, which leave 2^-22 of it out) from 0, then the groups
                     err = (kk[lo:hi].abs() @ qq.abs()) * (72 * 2.0 ** -23 + 2.0 ** -22)
@@ -75,7 +74,9 @@ def bound(out, spread, slack, dtype, n, vmax, blocks=False):
         weight = 2 * 2.0 ** -11      # p to fp16, p * s to fp16 (blocks: the value to fp16)
         last = 2.0 ** -8             # the output
         # sums of w u (u <= 15) and of 8 w: at most spread + 2 * 8 * s, s <= vmax / 8
-        sums = steps * 2.0 ** -23 * (spread + (0 if blocks else 2 * vmax)) * (4 if blocks else 1)   # (blocks: one sum over all rows)
+        sums = steps * 2.0 ** -23 * (spread + 2 * vmax)
+        if blocks:                   # the values themselves, one sum over all rows
+            sums = sums + n * 2.0 ** -23 * spread
     else:
         weight = 2 * 2.0 ** -21      # two fp16 numbers each
         last = 2.0 ** -24

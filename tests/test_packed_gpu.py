@@ -242,7 +242,8 @@ def test_blocks_of_queries_over_values_of_any_size(spread):
 
 def test_blocks_over_long_caches():
     for d in (64, 128):
-        check_attend(1, 2, 1, d, 70, 3000, [2999], [100], "bf16", seed=33)
+        for expected in (0, 200):      # the length that a call expects decides which kernel takes it
+            check_attend(1, 2, 1, d, 70, 3000, [2999], [100], "bf16", seed=33, split=expected)
 
 
 def test_blocks_meet_rows_that_are_not_finite():
