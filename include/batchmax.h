@@ -416,6 +416,9 @@ int32_t bm_last_prefill_path(void);
 /* Which kernel the calling thread's last bm_decode_step used.  fp32: 0 = a CTA per cache, 1 = clusters that share a cache.  bf16: 2 = a
  * CTA per cache, 3 = the same with all of K in registers, 4 = the stream, 5 = the stream over clusters that share a cache. */
 int32_t bm_last_decode_path(void);
+/* Which kernel the calling thread's last bm_packed_attend used: 0 = warps that share the caches' tiles, 1 = tiles of 128 query rows on
+ * the tensor cores (bf16, many query rows). */
+int32_t bm_last_packed_path(void);
 const char* bm_status_string(bm_status_t s);
 /* Text of the CUDA error behind the calling thread's most recent BM_ERR_CUDA from a kernel launch ("no error" if
  * none).  After BM_ERR_CUDA the state of the call's sample range is undefined: some of the call's kernels may have

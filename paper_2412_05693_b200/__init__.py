@@ -21,6 +21,7 @@ from .binding import (  # noqa: F401
 from .packed import (  # noqa: F401
     PackedCache,
     PackedConfig,
+    last_packed_path,
     packed_arena_bytes,
     packed_bytes_per_sample,
     packed_max_batch,

@@ -97,6 +97,7 @@ SIGNATURES = {
     "bm_kernel_launch_count": (C.c_uint64, []),
     "bm_last_prefill_path": (_i32, []),
     "bm_last_decode_path": (_i32, []),
+    "bm_last_packed_path": (_i32, []),
     "bm_status_string": (C.c_char_p, [_i32]),
     "bm_last_cuda_error": (C.c_char_p, []),
 }

@@ -5,6 +5,10 @@
 #include "../../include/batchmax.h"
 #include "packed.cuh"
 
+namespace bm {
+thread_local int g_last_packed_path = 0;
+}  // namespace bm
+
 using namespace bm;
 
 struct bm_packed {
@@ -218,6 +222,8 @@ bm_status_t bm_packed_attend(bm_packed_t* c, int32_t layer, int32_t sample0, int
   return status_of(launch_packed_attend(c->cfg.dtype, c->cfg.head_dim, view_of(c, layer, sample0, nsamples), a,
                                         static_cast<cudaStream_t>(cuda_stream)));
 }
+
+int32_t bm_last_packed_path(void) { return g_last_packed_path; }
 
 bm_status_t bm_packed_status(bm_packed_t* c, int32_t* device_status, void* cuda_stream) {
   if (c == nullptr || device_status == nullptr) return BM_ERR_INVALID;

@@ -38,6 +38,7 @@ namespace bm {
 namespace {
 
 constexpr int kWarps = 2;                     // independent of each other; one per CTA would cost 1 KB of shared memory more for each
+constexpr int kWarpsPerSm = 12;
 constexpr int kMostSms = 148;                 // that the workspace is sized for
 constexpr int kFullShift = 12;
 
@@ -127,25 +128,27 @@ struct AttendArgs {
   const int32_t* first;
   void* out;
   float mul;              // scale * log2(e)
-  int32_t query_tiles;    // of 8 NT query rows, per cache
+  int32_t query_tiles;    // of 8 (PAIR: 4) query rows, per cache
   int32_t runs;           // the most there may be: one for each warp of the grid
   int32_t slot_cols;      // query rows of a share in the workspace
   FastDiv by_g, by_query_tiles;
-  long long* before;      // workspace: [nsamples + 1] tiles (of one kv-head and query tile) of the samples before each
+  int32_t* before;        // workspace: [nsamples + 1] tiles (of one kv-head and query tile) of the samples before each
   float* partial;         // workspace: [runs][2][slot_cols][D + 4] sums of a cache's share, their maximum and sum of weights
 };
 
-// NT tiles of 8 columns.  PAIR: up to four query rows as 8-bit integers, each with two columns in Q.K and one of two in P.V (the other's
-// weights are 0).
-template <typename T, int D, int NT, bool PAIR>
+// PAIR: up to four query rows as 8-bit integers, each with two columns in Q.K and one of two in P.V (the other's weights are 0); else eight.
+// Wider tiles of query rows unpack less often and hold more: two and four times as many columns were no faster with bf16 at 16 rows of a
+// cache (16 samples of 4096 rows, 8 kv-heads, d = 128: 40 us, 42 now) and slower at 32 (93 against 60; fp32 204 against 109).
+template <typename T, int D, bool PAIR>
 struct Attend {
   static constexpr bool kSigned = sizeof(T) == 4;   // fp32: the MMAs take codes, not codes + 8
-  static constexpr int G = D / kPackedGroup, kPieces = kSigned ? 2 : 1, kCols = PAIR ? 4 : 8 * NT;
-  static constexpr int kStages = NT == 1 ? 3 : 2, kResident = NT == 1 ? 12 : 8;   // slots of the ring, warps per SM
-  static constexpr int kQueryWords = kSigned ? 8 * G : PAIR ? 2 * G : 4 * G;   // B fragments of Q for 8 columns, words of a lane
-  static constexpr int kQuery = NT > 1 ? NT * kQueryWords * 32 * 4 : 0;        // in shared memory where registers do not hold them
-  static constexpr int kWarpBytes = kStages * PackedLayout<D>::kBytes + kQuery, kSmem = kWarps * kWarpBytes;
-  static_assert(!PAIR || (NT == 1 && !kSigned), "");
+  static constexpr int G = D / kPackedGroup, kPieces = kSigned ? 2 : 1, kCols = PAIR ? 4 : 8;
+  // Slots of the ring, warps per SM.  us, 384 samples of 1535 rows, 32 / 8 heads, d = 128, with 16 warps of 128 registers 142, 14 167, 12 of 168
+  // 122, 10 137; four slots 121 against 118.
+  static constexpr int kStages = 3, kResident = kWarpsPerSm;
+  static constexpr int kQueryWords = kSigned ? 8 * G : PAIR ? 2 * G : 4 * G;   // B fragments of Q, words of a lane
+  static constexpr int kWarpBytes = kStages * PackedLayout<D>::kBytes, kSmem = kWarps * kWarpBytes;
+  static_assert(!PAIR || !kSigned, "");
 };
 
 // The rows of a sample that some query sees: tiles first .. first + n - 1 of its caches.
@@ -213,9 +216,9 @@ __device__ __forceinline__ void store4(T* p, float x, float y, float z, float w)
   }
 }
 
-template <typename T, int D, int NT, bool PAIR>
-__global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident / kWarps) packed_attend_kernel(AttendArgs a) {
-  using A = Attend<T, D, NT, PAIR>;
+template <typename T, int D, bool PAIR>
+__global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / kWarps) packed_attend_kernel(AttendArgs a) {
+  using A = Attend<T, D, PAIR>;
   using L = PackedLayout<D>;
   constexpr int G = A::G, P = A::kPieces, kStages = A::kStages, C = PAIR ? 1 : 2;   // C: columns of the sums that a lane has
   constexpr bool kSigned = A::kSigned;
@@ -243,10 +246,11 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
   int tiles_of_lane = 0;
 #pragma unroll 4
   for (int i = 0; i < each_lane; ++i) tiles_of_lane += tiles_at(mine0 + i);
-  const long long up_to_lane = warp_inclusive_sum((long long)tiles_of_lane, lane), total = __shfl_sync(0xffffffffu, up_to_lane, 31);
-  const long long all = total * per_sample;
+  // (the tiles of one kv-head of all samples fit 32 bits: 2^31 of them are 8 TB)
+  const int up_to_lane = warp_inclusive_sum(tiles_of_lane, lane), total = __shfl_sync(0xffffffffu, up_to_lane, 31);
+  const long long all = (long long)total * per_sample;
   if (run == 0) {   // for packed_combine_kernel
-    long long sum = up_to_lane - tiles_of_lane;
+    int sum = up_to_lane - tiles_of_lane;
     for (int smp = mine0; smp < min(mine0 + each_lane, ns); ++smp) {
       a.before[smp] = sum;
       sum += tiles_at(smp);
@@ -260,26 +264,30 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
   int left = (int)(cut.start(run + 1) - begin), to_issue = left;
   Walk at;
   {
-    const int src = __ffs(__ballot_sync(0xffffffffu, begin < up_to_lane * per_sample)) - 1;   // the lane whose samples `begin` falls to
-    long long before = __shfl_sync(0xffffffffu, up_to_lane - tiles_of_lane, src);
-    for (int s0 = src * each_lane;; s0 += 32) {
-      const int n = s0 + lane < (src + 1) * each_lane ? tiles_at(s0 + lane) : 0;
-      const long long up_to = before + warp_inclusive_sum(n, lane);
-      const unsigned hit = __ballot_sync(0xffffffffu, begin < up_to * per_sample);
-      if (hit != 0) {
-        const int k = __ffs(hit) - 1;
-        at.smp = s0 + k;
-        at.n = __shfl_sync(0xffffffffu, n, k);
-        at.first = sample_tiles(a, at.smp).first;
-        const long long in = begin - __shfl_sync(0xffffffffu, up_to - n, k) * per_sample;
-        const int unit = (unsigned long long)in >> 32 ? (int)(in / at.n) : (int)((uint32_t)in / (uint32_t)at.n);
-        at.t = (int)(in - (long long)unit * at.n);
-        at.head = a.by_query_tiles(unit);
-        at.qt = unit - at.head * a.query_tiles;
-        break;
+    const int src = __ffs(__ballot_sync(0xffffffffu, begin < (long long)up_to_lane * per_sample)) - 1;   // the lane whose samples `begin` is in
+    int before = __shfl_sync(0xffffffffu, up_to_lane - tiles_of_lane, src);
+    at.smp = src;
+    at.n = __shfl_sync(0xffffffffu, tiles_of_lane, src);
+    if (each_lane > 1) {
+      for (int s0 = src * each_lane;; s0 += 32) {
+        const int n = s0 + lane < (src + 1) * each_lane ? tiles_at(s0 + lane) : 0, up_to = before + warp_inclusive_sum(n, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, begin < (long long)up_to * per_sample);
+        if (hit != 0) {
+          const int k = __ffs(hit) - 1;
+          at.smp = s0 + k;
+          at.n = __shfl_sync(0xffffffffu, n, k);
+          before = __shfl_sync(0xffffffffu, up_to - n, k);
+          break;
+        }
+        before = __shfl_sync(0xffffffffu, up_to, 31);
       }
-      before = __shfl_sync(0xffffffffu, up_to, 31);
     }
+    at.first = a.first != nullptr ? max(a.first[at.smp], 0) / kPackedTile : 0;
+    const long long in = begin - (long long)before * per_sample;
+    const int unit = (unsigned long long)in >> 32 ? (int)(in / at.n) : (int)((uint32_t)in / (uint32_t)at.n);
+    at.t = (int)(in - (long long)unit * at.n);
+    at.head = a.by_query_tiles(unit);
+    at.qt = unit - at.head * a.query_tiles;
   }
   Walk ahead = at;   // the next tile to fetch
   const uint8_t* from = nullptr;
@@ -307,25 +315,19 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
   uint32_t parity = 0;
 #pragma unroll 1
   while (left > 0) {
-    // ---- one cache's share: its queries, lane (r, c) has the elements 32 g + 8 c .. + 7 of column 8 nt + r ---------------------
+    // ---- one cache's share: its queries, lane (r, c) has the elements 32 g + 8 c .. + 7 of its column -----------------------
     const Tiles sample = sample_tiles(a, at.smp);
     const int len = sample.len, lo = sample.lo, share = min(at.n - at.t, left), col0 = at.qt * A::kCols;
     const int cols_here = min(A::kCols, cols - col0);
     // query i sees the rows [lo, len - (I - 1 - i)); the first of this tile's the rows below `least`, the last those below `most_rows`
     const int least = len - (a.I - 1 - a.by_g(col0)), most_rows = len - (a.I - 1 - a.by_g(col0 + cols_here - 1));
-    uint32_t bq[NT == 1 ? A::kQueryWords : 1];   // [number][group][two k-steps][b0, b1], integers: [group][b0, b1]
-    uint32_t* bq_smem = reinterpret_cast<uint32_t*>(ring + kStages * L::kBytes);   // [nt][pair of words][lane][2]
-    uint32_t start[NT];                          // B fragment of the -8 sum q: two fp16 numbers for each group
+    uint32_t bq[A::kQueryWords];                 // [number][group][two k-steps][b0, b1], integers: [group][b0, b1]
+    uint32_t start = 0;                          // B fragment of the -8 sum q: two fp16 numbers for each group
     int start_int[PAIR ? G : 1][2];              // -8 sum of hi, of lo, of this lane's column
-    float colmul[NT][C];                         // of this lane's columns
+    float colmul[C];                             // of this lane's columns
     [[maybe_unused]] float not_finite = 0.f;     // integers: NaN where the column's query is not finite
-    auto put_query = [&](int nt, int k, uint32_t w) {
-      if constexpr (NT == 1) bq[k] = w;
-      else bq_smem[((nt * (A::kQueryWords / 2) + k / 2) * 32 + lane) * 2 + k % 2] = w;
-    };
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int col = col0 + (PAIR ? r / 2 : 8 * nt + r), query = a.by_g(col);
+    {
+      const int col = col0 + (PAIR ? r / 2 : r), query = a.by_g(col);
       const T* q = static_cast<const T*>(a.q) + at.smp * a.q_sample + query * a.q_token + ((size_t)at.head * a.c.g + col - query * a.c.g) * D + 8 * c;
       float x[G][8];
       uint32_t most_bits = 0;   // magnitudes compare as integers, what is not finite above the rest
@@ -362,7 +364,7 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
 #pragma unroll
             for (int j = 0; j < 4; ++j) y[j] = __float_as_uint(fmaf(x[gi][2 * j + odd], up, magic));
             const uint32_t b = __byte_perm(__byte_perm(y[0], y[1], two), __byte_perm(y[2], y[3], two), 0x5410);
-            put_query(nt, gi * 2 + odd, b);
+            bq[gi * 2 + odd] = b;
             sum = __dp4a((int)b, 0x01010101, sum);
           }
           sum += __shfl_xor_sync(0xffffffffu, sum, 1);
@@ -387,14 +389,13 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               const float by = k % 2 ? kOdd / kEven : 1.f;
-              put_query(nt, (pc * G + gi) * 4 + k, pack(v[pc][k] * by, v[pc][k + 4] * by));
+              bq[(pc * G + gi) * 4 + k] = pack(v[pc][k] * by, v[pc][k + 4] * by);
             }
           sum += __shfl_xor_sync(0xffffffffu, sum, 1);
           sum += __shfl_xor_sync(0xffffffffu, sum, 2);
           sums[gi] = sum * (-8.f / kKey);
         }
         // k = 2 c, 2 c + 1 of the start's MMA: the groups 0 .. G - 1 of the first fp16 number, then those of the second
-        start[nt] = 0;
 #pragma unroll
         for (int k = 0; k < 2 * G; k += 2) {
           float s0 = sums[k % G], s1 = sums[k % G + 1];
@@ -402,50 +403,46 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
             s0 -= __half2float(__float2half_rn(s0));
             s1 -= __half2float(__float2half_rn(s1));
           }
-          if (c == k / 2) start[nt] = pack(s0, s1);
+          if (c == k / 2) start = pack(s0, s1);
         }
       }
 #pragma unroll
-      for (int j = 0; j < C; ++j) colmul[nt][j] = __shfl_sync(0xffffffffu, mul, 4 * (2 * c + j));   // from this lane's column to the sums'
+      for (int j = 0; j < C; ++j) colmul[j] = __shfl_sync(0xffffffffu, mul, 4 * (2 * c + j));   // from this lane's column to the sums'
     }
-    auto column = [&](int nt, int j) { return PAIR ? c : 8 * nt + 2 * c + j; };   // of the sums, from col0
-    if constexpr (NT > 1) __syncwarp();
+    auto column = [&](int j) { return PAIR ? c : 2 * c + j; };   // of the sums, from col0
 
-    float m[NT][C], mneg[NT][C], l[NT][C], o[NT][G][2][4], ow[NT][4];   // mneg = shift - m
+    float m[C], mneg[C], l[C], o[G][2][4], ow[4];   // mneg = shift - m
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int j = 0; j < C; ++j) {
-        m[nt][j] = -INFINITY;
-        mneg[nt][j] = l[nt][j] = 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) ow[nt][k] = 0.f;
-#pragma unroll
-      for (int gi = 0; gi < G; ++gi)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[nt][gi][k / 4][k % 4] = 0.f;
+    for (int j = 0; j < C; ++j) {
+      m[j] = -INFINITY;
+      mneg[j] = l[j] = 0.f;
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) ow[k] = 0.f;
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[gi][k / 4][k % 4] = 0.f;
     int shift = kFullShift;
     [[maybe_unused]] int lift = kSigned ? 15 : 0;   // fp32: the value scales are taken times 2^lift, so that small ones keep their second number
     auto over_of = [](int total) { return 0x7fff7fffu - 0x00010001u * (((28 - total) << 10) - 1); };
     uint32_t over_add = over_of(shift + lift);      // carries into bit 15 what is 2^(13 - shift - lift) or more
 
-    auto rescale_outputs = [&](int nt, const float* k) {
+    auto rescale_outputs = [&](const float* k) {
 #pragma unroll
       for (int gi = 0; gi < G; ++gi)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int j = 0; j < C; ++j) o[nt][gi][i / 2][2 * (i % 2) + j] *= k[j];
+          for (int j = 0; j < C; ++j) o[gi][i / 2][2 * (i % 2) + j] *= k[j];
     };
-    auto rescale = [&](int nt, const float* k) {   // everything that was summed with the weights
+    auto rescale = [&](const float* k) {   // everything that was summed with the weights
 #pragma unroll
       for (int j = 0; j < C; ++j) {
-        l[nt][j] *= k[j];
-        if constexpr (!kSigned) ow[nt][j] *= k[j];
+        l[j] *= k[j];
+        if constexpr (!kSigned) ow[j] *= k[j];
       }
-      rescale_outputs(nt, k);
+      rescale_outputs(k);
     };
 
     auto tile = [&](auto masked_tag, int row0, unsigned char* in) {
@@ -470,16 +467,14 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
             if (bad != 0) {
               if (bad >> lane & 1) *place = 0;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
+              for (int j = 0; j < C; ++j) {
+                const int seen = len - (a.I - 1 - a.by_g(col0 + column(j)));
+                const int b0 = max(lo - row0, 0), b1 = min(seen - row0, 32);
+                const uint32_t rows = b1 > b0 ? (0xffffffffu >> (32 - (b1 - b0))) << b0 : 0u;
+                if (bad & rows)
 #pragma unroll
-                for (int j = 0; j < C; ++j) {
-                  const int seen = len - (a.I - 1 - a.by_g(col0 + column(nt, j)));
-                  const int b0 = max(lo - row0, 0), b1 = min(seen - row0, 32);
-                  const uint32_t rows = b1 > b0 ? (0xffffffffu >> (32 - (b1 - b0))) << b0 : 0u;
-                  if (bad & rows)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[nt][gi][i / 2][2 * (i % 2) + j] = __int_as_float(0x7fffffff);
-                }
+                  for (int i = 0; i < 4; ++i) o[gi][i / 2][2 * (i % 2) + j] = __int_as_float(0x7fffffff);
+              }
             }
           }
           largest = __reduce_max_sync(0xffffffffu, largest);
@@ -489,14 +484,11 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
             const float k = pow2(next_shift - shift), k_lift = pow2(next - next_shift - lift);
             const float ks[2] = {k, k};
             [[maybe_unused]] const float ks_lift[2] = {k_lift, k_lift};
+            rescale(ks);
+            if constexpr (kSigned) rescale_outputs(ks_lift);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              rescale(nt, ks);
-              if constexpr (kSigned) rescale_outputs(nt, ks_lift);
-#pragma unroll
-              for (int j = 0; j < C; ++j)
-                if (m[nt][j] != -INFINITY) mneg[nt][j] = (float)next_shift - m[nt][j];
-            }
+            for (int j = 0; j < C; ++j)
+              if (m[j] != -INFINITY) mneg[j] = (float)next_shift - m[j];
             shift = next_shift;
             lift = next - next_shift;
             over_add = over_of(next);
@@ -507,7 +499,7 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
       }
 
       // ---- logits -------------------------------------------------------------------------------------------------------------
-      float s[2][NT][2][C];   // [16 keys][column tile][key + 8][column]
+      float s[2][2][C];   // [16 keys][key + 8][column]
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
         // the MMA's row r is the key r / 2 + 4 (r % 2), so that a lane's four keys in P.V are c, c + 4, c + 8, c + 12
@@ -517,17 +509,14 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
         lds<G>(in + (key + 8) * (D / 2) + c * 4 * G, w1);
         lds<G / 2>(in + L::kKeyScales + key * G * 2, sc[0]);
         lds<G / 2>(in + L::kKeyScales + (key + 8) * G * 2, sc[1]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float first[4] = {0.f, 0.f, 0.f, 0.f};
-          if constexpr (!kSigned && !PAIR) {   // (G = 2: lanes c >= 2 multiply by 0)
-            mma_k8(first, G == 4 && (c & 1) ? sc[0][G / 2 - 1] : sc[0][0], G == 4 && (c & 1) ? sc[1][G / 2 - 1] : sc[1][0], start[nt]);
-          }
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int j = 0; j < C; ++j) s[sub][nt][k][j] = first[2 * k + j];
+        float first[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (!kSigned && !PAIR) {   // (G = 2: lanes c >= 2 multiply by 0)
+          mma_k8(first, G == 4 && (c & 1) ? sc[0][G / 2 - 1] : sc[0][0], G == 4 && (c & 1) ? sc[1][G / 2 - 1] : sc[1][0], start);
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int j = 0; j < C; ++j) s[sub][k][j] = first[2 * k + j];
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) {
           const float2 p0 = unpack(sc[0][gi / 2]), p1 = unpack(sc[1][gi / 2]);
@@ -537,33 +526,24 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
             int acc[4];
             mma_u8s8(acc, a0, bq[2 * gi], bq[2 * gi + 1], start_int[gi][0], start_int[gi][1]);
             // |sum code q| < 32 * 8 * 2^14 = 2^22
-            s[sub][0][0][0] = fmaf(s0, __int_as_float(acc[0] * 256 + acc[1]) - __int_as_float(kMagic), s[sub][0][0][0]);
-            s[sub][0][1][0] = fmaf(s1, __int_as_float(acc[2] * 256 + acc[3]) - __int_as_float(kMagic), s[sub][0][1][0]);
+            s[sub][0][0] = fmaf(s0, __int_as_float(acc[0] * 256 + acc[1]) - __int_as_float(kMagic), s[sub][0][0]);
+            s[sub][1][0] = fmaf(s1, __int_as_float(acc[2] * 256 + acc[3]) - __int_as_float(kMagic), s[sub][1][0]);
           } else {
             const uint32_t x0 = w0[gi] >> 8, x1 = w1[gi] >> 8;
             const uint32_t a0[4] = {codes<kSigned, false>(w0[gi]), codes<kSigned, false>(w1[gi]), codes<kSigned, true>(w0[gi]),
                                     codes<kSigned, true>(w1[gi])};
             const uint32_t a1[4] = {codes<kSigned, false>(x0), codes<kSigned, false>(x1), codes<kSigned, true>(x0), codes<kSigned, true>(x1)};
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              auto query = [&](int k, uint32_t* b) {   // the k-th pair of words
-                if constexpr (NT == 1) { b[0] = bq[2 * k]; b[1] = bq[2 * k + 1]; }
-                else lds<2>(bq_smem + ((nt * (A::kQueryWords / 2) + k) * 32 + lane) * 2, b);
-              };
-              float acc[4] = {0.f, 0.f, 0.f, 0.f};
-              uint32_t b[2];
+            for (int pc = 0; pc < P; ++pc) {
+              const uint32_t* b = bq + (pc * G + gi) * 4;
+              mma(acc, a0, b[0], b[1], acc);
+              mma(acc, a1, b[2], b[3], acc);
+            }
 #pragma unroll
-              for (int pc = 0; pc < P; ++pc) {
-                query((pc * G + gi) * 2, b);
-                mma(acc, a0, b[0], b[1], acc);
-                query((pc * G + gi) * 2 + 1, b);
-                mma(acc, a1, b[0], b[1], acc);
-              }
-#pragma unroll
-              for (int j = 0; j < C; ++j) {
-                s[sub][nt][0][j] = fmaf(s0, acc[j], s[sub][nt][0][j]);
-                s[sub][nt][1][j] = fmaf(s1, acc[2 + j], s[sub][nt][1][j]);
-              }
+            for (int j = 0; j < C; ++j) {
+              s[sub][0][j] = fmaf(s0, acc[j], s[sub][0][j]);
+              s[sub][1][j] = fmaf(s1, acc[2 + j], s[sub][1][j]);
             }
           }
         }
@@ -571,62 +551,55 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
 
       // ---- softmax, running -----------------------------------------------------------------------------------------------------
       bool grown = false;
-      float top[NT][C];
+      float top[C];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int j = 0; j < C; ++j) {
+        if constexpr (kMasked) {
+          const int seen = len - (a.I - 1 - a.by_g(col0 + column(j)));
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int row = row0 + sub * 16 + 8 * k + r / 2 + 4 * (r % 2);
+              if (row < lo || row >= seen) s[sub][k][j] = -INFINITY;
+            }
+        }
+        top[j] = fmaxf(fmaxf(s[0][0][j], s[0][1][j]), fmaxf(s[1][0][j], s[1][1][j])) * colmul[j];
+        grown |= top[j] > m[j] + 2.f;
+      }
+      if (__any_sync(0xffffffffu, grown)) {
+        float k[C];
 #pragma unroll
         for (int j = 0; j < C; ++j) {
-          if constexpr (kMasked) {
-            const int seen = len - (a.I - 1 - a.by_g(col0 + column(nt, j)));
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int row = row0 + sub * 16 + 8 * k + r / 2 + 4 * (r % 2);
-                if (row < lo || row >= seen) s[sub][nt][k][j] = -INFINITY;
-              }
-          }
-          top[nt][j] = fmaxf(fmaxf(s[0][nt][0][j], s[0][nt][1][j]), fmaxf(s[1][nt][0][j], s[1][nt][1][j])) * colmul[nt][j];
-          grown |= top[nt][j] > m[nt][j] + 2.f;
+          float t = top[j];
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
+          t = fmaxf(m[j], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16)));
+          k[j] = m[j] == t ? 1.f : exp2_approx(m[j] - t);   // (both -inf: nothing seen yet)
+          m[j] = t;
+          mneg[j] = t == -INFINITY ? 0.f : (float)shift - t;
         }
-      if (__any_sync(0xffffffffu, grown)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float k[C];
-#pragma unroll
-          for (int j = 0; j < C; ++j) {
-            float t = top[nt][j];
-            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
-            t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
-            t = fmaxf(m[nt][j], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16)));
-            k[j] = m[nt][j] == t ? 1.f : exp2_approx(m[nt][j] - t);   // (both -inf: nothing seen yet)
-            m[nt][j] = t;
-            mneg[nt][j] = t == -INFINITY ? 0.f : (float)shift - t;
-          }
-          rescale(nt, k);
-        }
+        rescale(k);
       }
       // weights p * 2^shift: lane (r, c) ends with the column r and the keys c, c + 4 (b0) and c + 8, c + 12 (b1) of every 16
-      uint32_t w[2][NT][P][2];
+      uint32_t w[2][P][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
+        for (int k = 0; k < 2; ++k) {
+          float p[2] = {0.f, 0.f};
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            float p[2] = {0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-              p[j] = exp2_approx(fmaf(s[sub][nt][k][j], colmul[nt][j], mneg[nt][j]));
-              l[nt][j] += p[j];
-            }
-            const uint32_t h = pack(p[0], p[1]);
-            w[sub][nt][0][k] = transpose8x8(h);
-            if constexpr (P == 2) {
-              const float2 back = unpack(h);
-              w[sub][nt][P - 1][k] = transpose8x8(pack(p[0] - back.x, p[1] - back.y));
-            }
+          for (int j = 0; j < C; ++j) {
+            p[j] = exp2_approx(fmaf(s[sub][k][j], colmul[j], mneg[j]));
+            l[j] += p[j];
           }
+          const uint32_t h = pack(p[0], p[1]);
+          w[sub][0][k] = transpose8x8(h);
+          if constexpr (P == 2) {
+            const float2 back = unpack(h);
+            w[sub][P - 1][k] = transpose8x8(pack(p[0] - back.x, p[1] - back.y));
+          }
+        }
 
       // ---- outputs ---------------------------------------------------------------------------------------------------------------
       [[maybe_unused]] const float lifted = pow2(lift);
@@ -640,12 +613,10 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
         }
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
-        float part[kSigned ? NT : 1][2][4];
+        float part[2][4];
         if constexpr (kSigned) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) part[nt][i / 4][i % 4] = 0.f;
+          for (int i = 0; i < 8; ++i) part[i / 4][i % 4] = 0.f;
         }
 #pragma unroll
         for (int sub = 0; sub < 2; ++sub) {
@@ -654,35 +625,30 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
           const uint32_t a1[4] = {codes<kSigned, false>(y0), codes<kSigned, true>(y0), codes<kSigned, false>(y1), codes<kSigned, true>(y1)};
           [[maybe_unused]] const uint32_t ones = r == gi ? 0x3c003c00u : 0u;
           [[maybe_unused]] const uint32_t a2[4] = {ones, 0u, ones, 0u};   // row gi: the sum of the weights
+          uint32_t b[P][2];
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            uint32_t b[P][2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              if constexpr (P == 1) {
-                b[0][k] = mul2(w[sub][nt][0][k], sv[sub][k][gi]);
-              } else {
-                const float2 hi2 = unpack(w[sub][nt][0][k]), lo2 = unpack(w[sub][nt][P - 1][k]), s2 = unpack(sv[sub][k][gi]);
-                const float y0f = (hi2.x + lo2.x) * (s2.x * lifted), y1f = (hi2.y + lo2.y) * (s2.y * lifted);
-                b[0][k] = pack(y0f, y1f);
-                const float2 back = unpack(b[0][k]);
-                b[P - 1][k] = pack(y0f - back.x, y1f - back.y);
-              }
+          for (int k = 0; k < 2; ++k) {
+            if constexpr (P == 1) {
+              b[0][k] = mul2(w[sub][0][k], sv[sub][k][gi]);
+            } else {
+              const float2 hi2 = unpack(w[sub][0][k]), lo2 = unpack(w[sub][P - 1][k]), s2 = unpack(sv[sub][k][gi]);
+              const float y0f = (hi2.x + lo2.x) * (s2.x * lifted), y1f = (hi2.y + lo2.y) * (s2.y * lifted);
+              b[0][k] = pack(y0f, y1f);
+              const float2 back = unpack(b[0][k]);
+              b[P - 1][k] = pack(y0f - back.x, y1f - back.y);
             }
-            float(&to)[2][4] = *(kSigned ? &part[kSigned ? nt : 0] : &o[nt][gi]);
+          }
+          float(&to)[2][4] = kSigned ? part : o[gi];
 #pragma unroll
-            for (int pc = 0; pc < P; ++pc) {
-              mma(to[0], a0, b[pc][0], b[pc][1], to[0]);
-              mma(to[1], a1, b[pc][0], b[pc][1], to[1]);
-              if constexpr (!kSigned) mma(ow[nt], a2, b[pc][0], b[pc][1], ow[nt]);
-            }
+          for (int pc = 0; pc < P; ++pc) {
+            mma(to[0], a0, b[pc][0], b[pc][1], to[0]);
+            mma(to[1], a1, b[pc][0], b[pc][1], to[1]);
+            if constexpr (!kSigned) mma(ow, a2, b[pc][0], b[pc][1], ow);
           }
         }
         if constexpr (kSigned) {
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) o[nt][gi][i / 4][i % 4] += part[nt][i / 4][i % 4];
+          for (int i = 0; i < 8; ++i) o[gi][i / 4][i % 4] += part[i / 4][i % 4];
         }
       }
     };
@@ -710,30 +676,27 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, NT, PAIR>::kResident
     const bool whole = share == at.n;
     float* to = a.partial + ((size_t)run * 2 + (at.t == 0 ? 1 : 0)) * a.slot_cols * (D + 4);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    for (int j = 0; j < C; ++j) {
+      l[j] += __shfl_xor_sync(0xffffffffu, l[j], 4);
+      l[j] += __shfl_xor_sync(0xffffffffu, l[j], 8);
+      l[j] += __shfl_xor_sync(0xffffffffu, l[j], 16);
+      if constexpr (PAIR)
+        if (l[j] != 0.f) l[j] += not_finite;   // (seen something)
+      const int cc = column(j), col = col0 + cc, query = a.by_g(col);
+      const float by = (whole ? (l[j] == 0.f ? 0.f : 1.f / l[j]) : 1.f) * pow2(-lift);   // (a query that sees no row has a row of zeros)
+      T* out = static_cast<T*>(a.out) + (((size_t)at.smp * a.I + query) * a.c.Hq + (size_t)at.head * a.c.g + col - query * a.c.g) * D + 4 * r;
 #pragma unroll
-      for (int j = 0; j < C; ++j) {
-        l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], 4);
-        l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], 8);
-        l[nt][j] += __shfl_xor_sync(0xffffffffu, l[nt][j], 16);
-        if constexpr (PAIR)
-          if (l[nt][j] != 0.f) l[nt][j] += not_finite;   // (seen something)
-        const int cc = column(nt, j), col = col0 + cc, query = a.by_g(col);
-        const float by = (whole ? (l[nt][j] == 0.f ? 0.f : 1.f / l[nt][j]) : 1.f) * pow2(-lift);   // (a query that sees no row has a row of zeros)
-        T* out = static_cast<T*>(a.out) + (((size_t)at.smp * a.I + query) * a.c.Hq + (size_t)at.head * a.c.g + col - query * a.c.g) * D + 4 * r;
-#pragma unroll
-        for (int gi = 0; gi < G; ++gi) {
-          const float sum = kSigned ? 0.f : 8.f * __shfl_sync(0xffffffffu, ow[nt][j], 4 * gi + c);
-          const float x0 = (o[nt][gi][0][j] * kEven - sum) * by, x1 = (o[nt][gi][0][2 + j] * kOdd - sum) * by;
-          const float x2 = (o[nt][gi][1][j] * kEven - sum) * by, x3 = (o[nt][gi][1][2 + j] * kOdd - sum) * by;
-          if (cc < cols_here) {
-            if (whole) store4(out + 32 * gi, x0, x1, x2, x3);
-            else store4(to + cc * (D + 4) + 32 * gi + 4 * r, x0, x1, x2, x3);
-          }
+      for (int gi = 0; gi < G; ++gi) {
+        const float sum = kSigned ? 0.f : 8.f * __shfl_sync(0xffffffffu, ow[j], 4 * gi + c);
+        const float x0 = (o[gi][0][j] * kEven - sum) * by, x1 = (o[gi][0][2 + j] * kOdd - sum) * by;
+        const float x2 = (o[gi][1][j] * kEven - sum) * by, x3 = (o[gi][1][2 + j] * kOdd - sum) * by;
+        if (cc < cols_here) {
+          if (whole) store4(out + 32 * gi, x0, x1, x2, x3);
+          else store4(to + cc * (D + 4) + 32 * gi + 4 * r, x0, x1, x2, x3);
         }
-        // the weights are 2^shift times p to the maximum m
-        if (!whole && r == 0 && cc < cols_here) *reinterpret_cast<float2*>(to + cc * (D + 4) + D) = make_float2(m[nt][j] - (float)shift, l[nt][j]);
       }
+      // the weights are 2^shift times p to the maximum m
+      if (!whole && r == 0 && cc < cols_here) *reinterpret_cast<float2*>(to + cc * (D + 4) + D) = make_float2(m[j] - (float)shift, l[j]);
     }
     left -= share;
     if (left > 0) at.next_cache(a);
@@ -766,8 +729,9 @@ __global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_c
   const int g = a.c.g, cols = a.I * g, at = x * 4;
   if (i >= (long long)a.c.nsamples * a.c.Hkv * cols) return;   // (uniform where kGroups > 1)
   const int unit = (int)i / cols, col = (int)i % cols, qt = col / cols_per_tile, smp = unit / a.c.Hkv, head = unit % a.c.Hkv;
-  const long long per_sample = (long long)a.c.Hkv * a.query_tiles, all = a.before[a.c.nsamples] * per_sample;
-  const long long before = a.before[smp], n = a.before[smp + 1] - before;
+  const long long per_sample = (long long)a.c.Hkv * a.query_tiles;
+  const int before = a.before[smp], n = a.before[smp + 1] - before;
+  const long long all = a.before[a.c.nsamples] * per_sample;
   T* out = static_cast<T*>(a.out) + (((size_t)smp * a.I + col / g) * a.c.Hq + (size_t)head * g + col % g) * D + at;
   if (n == 0) {
     if (part == 0) store4(out, 0.f, 0.f, 0.f, 0.f);
@@ -812,13 +776,11 @@ __global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_c
   store4(out, mine.o.x * inv, mine.o.y * inv, mine.o.z * inv, mine.o.w * inv);
 }
 
-// Query rows that a warp takes, in units of 8.
-int column_tiles(int64_t cols) { return cols <= 8 ? 1 : cols <= 16 ? 2 : 4; }
-size_t before_bytes(int nsamples) { return ((size_t)nsamples + 1 + 31) / 32 * 32 * sizeof(long long); }
+size_t before_bytes(int nsamples) { return ((size_t)nsamples + 1 + 63) / 64 * 64 * sizeof(int32_t); }
 
-template <typename T, int D, int NT, bool PAIR>
-cudaError_t launch_nt(const AttendArgs& args, void* workspace, int max_len, cudaStream_t st) {
-  using A = Attend<T, D, NT, PAIR>;
+template <typename T, int D, bool PAIR>
+cudaError_t launch_columns(const AttendArgs& args, void* workspace, int max_len, cudaStream_t st) {
+  using A = Attend<T, D, PAIR>;
   AttendArgs a = args;
   const int64_t units = (int64_t)a.c.nsamples * a.c.Hkv, cols = (int64_t)a.I * a.c.g;
   a.query_tiles = (int)((cols + A::kCols - 1) / A::kCols);
@@ -827,11 +789,11 @@ cudaError_t launch_nt(const AttendArgs& args, void* workspace, int max_len, cuda
   a.slot_cols = (int)std::min<int64_t>(A::kCols, cols);
   a.by_g = FastDiv((uint32_t)a.c.g);
   a.by_query_tiles = FastDiv((uint32_t)a.query_tiles);
-  a.before = static_cast<long long*>(workspace);
+  a.before = static_cast<int32_t*>(workspace);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + before_bytes(a.c.nsamples));
   static SmemConfigured configured;
-  if (cudaError_t err = configured.ensure(packed_attend_kernel<T, D, NT, PAIR>, A::kSmem); err != cudaSuccess) return err;
-  cudaError_t err = launch_dependent(packed_attend_kernel<T, D, NT, PAIR>, dim3((a.runs + kWarps - 1) / kWarps), dim3(kWarps * 32), A::kSmem, st, a);
+  if (cudaError_t err = configured.ensure(packed_attend_kernel<T, D, PAIR>, A::kSmem); err != cudaSuccess) return err;
+  cudaError_t err = launch_dependent(packed_attend_kernel<T, D, PAIR>, dim3((a.runs + kWarps - 1) / kWarps), dim3(kWarps * 32), A::kSmem, st, a);
   count_launch();
   if (err != cudaSuccess) return err;
   const int64_t rows = units * cols;
@@ -854,31 +816,25 @@ cudaError_t launch_nt(const AttendArgs& args, void* workspace, int max_len, cuda
 
 template <typename T, int D>
 cudaError_t launch_t(const AttendArgs& a, void* workspace, int max_len, cudaStream_t st) {
-  switch (column_tiles((int64_t)a.I * a.c.g)) {
-    case 1:
-      if constexpr (sizeof(T) == 2)
-        if ((int64_t)a.I * a.c.g <= 4) return launch_nt<T, D, 1, true>(a, workspace, max_len, st);
-      return launch_nt<T, D, 1, false>(a, workspace, max_len, st);
-    case 2: return launch_nt<T, D, 2, false>(a, workspace, max_len, st);
-    default: return launch_nt<T, D, 4, false>(a, workspace, max_len, st);
-  }
+  // (five to eight query rows in two tiles of four would unpack everything twice)
+  if constexpr (sizeof(T) == 2)
+    if ((int64_t)a.I * a.c.g <= 4) return launch_columns<T, D, true>(a, workspace, max_len, st);
+  return launch_columns<T, D, false>(a, workspace, max_len, st);
 }
 
 }  // namespace
 
 size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles) {
-  // The most that a call of up to this size may take, whichever kernel column_tiles chooses for it: every run leaves two shares at most.
-  size_t most = 0;
-  for (int nt = 1; nt <= column_tiles((int64_t)queries * g); nt *= 2) {
-    const int64_t cols = std::min((int64_t)queries * g, (int64_t)(nt == 4 ? INT32_MAX : 8 * nt));
-    const int64_t all = (int64_t)batch * Hkv * ((cols + 8 * nt - 1) / (8 * nt)) * tiles;
-    most = std::max(most, (size_t)std::min(all, (int64_t)kMostSms * (nt == 1 ? 12 : 8)) * 2 * std::min<int64_t>(8 * nt, cols) * (d + 4) * sizeof(float));
-  }
+  // every run leaves two shares at most; calls of fewer samples, queries or rows take no more runs and no more columns
+  const int64_t cols = (int64_t)queries * g, all = (int64_t)batch * Hkv * ((cols + 3) / 4) * tiles;
+  const int64_t runs = std::min<int64_t>(all, kMostSms * kWarpsPerSm);
+  const size_t most = (size_t)runs * 2 * std::min<int64_t>(8, cols) * (d + 4) * sizeof(float);
   return std::max(before_bytes(batch) + most, packed_block_workspace(batch, Hkv));
 }
 
 cudaError_t launch_packed_attend(int dtype, int d, const PackedView& c, const PackedAttend& p, cudaStream_t st) {
-  if (dtype == 1 && packed_block_pays(d, c, p.I, p.max_len)) return launch_packed_block(d, c, p, st);
+  g_last_packed_path = dtype == 1 && packed_block_pays(d, c, p.I, p.max_len) ? 1 : 0;
+  if (g_last_packed_path == 1) return launch_packed_block(d, c, p, st);
   AttendArgs a;
   a.c = c;
   a.q = p.q; a.q_sample = p.q_sample; a.q_token = p.q_token;

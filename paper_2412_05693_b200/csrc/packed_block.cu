@@ -515,16 +515,15 @@ cudaError_t launch_d(const PackedView& c, const PackedAttend& p, cudaStream_t st
 
 }  // namespace
 
-// Which calls take this kernel: its time goes by rounds of one CTA per SM and 128 keys, that of the warps' kernel by tiles of 32 keys x 32
-// query rows, shared evenly, and what joining them costs.  us, this kernel / the other: 32 / 8 heads, d = 128, 16 samples of 4096 rows, 32
-// query rows of a cache 100 / 92, 64 rows 100 / 156, 128 rows 102 / 223; 4 samples, 64 rows 86 / 54, 128 rows 86 / 86, 1024 rows (4352) 103 /
-// 414; 1 sample of 4352, 256 rows 97 / 55, 1024 rows 98 / 148; of 16384, 512 rows 336 / 214; 64 samples of 1024, 64 rows 119 / 177; 32 samples
-// of 2048, 32 heads without groups, 16 rows 385 / 102, 64 rows 390 / 481; 8 heads, d = 64, 4 samples of 4352, 1024 rows 76 / 193.
+// Which calls take this kernel: its time goes by rounds of one CTA per SM and 128 keys, that of the warps' kernel by tiles of 32 keys x 8
+// query rows, shared evenly.  us, this kernel / the other: 32 / 8 heads, d = 128, 16 samples of 4096 rows, 32 query rows of a cache 100 /
+// 61, 64 rows 100 / 110, 128 rows 102 / 212; 4 samples, 64 rows 86 / 42, 128 rows 86 / 60, 256 rows 97 / 110, 1024 rows (4352) 103 / 432;
+// 1 sample of 4352, 256 rows 97 / 43, 1024 rows 98 / 115; of 16384, 512 rows 336 / 204; 64 samples of 1024, 64 rows 119 / 125; 32 samples of
+// 2048, 32 heads without groups, 64 rows 390 / 433; 8 kv-heads, d = 64, 4 samples of 4352, 1024 rows 76 / 264.
 bool packed_block_pays(int d, const PackedView& c, int I, int max_len) {
   const double cols = (double)I * c.g, units = (double)c.nsamples * c.Hkv, pairs = std::ceil(cols / (2 * kRows));
-  if (cols <= 32) return false;
   const double here = (d == 64 ? 2.1 : 2.75) * std::ceil(units * pairs / sm_count()) * max_len / kKeys;
-  const double warps = 40 + (d == 64 ? 1.3 : 3.1) * units * std::ceil(cols / 32) * max_len / kPackedTile / (8. * sm_count());
+  const double warps = (d == 64 ? 0.81 : 1.36) * units * std::ceil(cols / 8) * max_len / kPackedTile / (12. * sm_count());
   return here < warps;
 }
 

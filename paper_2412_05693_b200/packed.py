@@ -61,6 +61,11 @@ def packed_max_batch(cfg: PackedConfig, hbm_budget_bytes: int) -> int:
     return out.value
 
 
+def last_packed_path() -> int:
+    """0: warps that share the caches' tiles took this thread's last attend call, 1: tiles of 128 query rows did."""
+    return int(lib().bm_last_packed_path())
+
+
 class PackedCache:
     """Handle of one bm_packed_t plus the torch tensors backing its arena and the workspace of its attend calls.
 

@@ -39,31 +39,33 @@ def attend(q, k, v, lens, first, scale, dtype, blocks=False):
     spread = torch.zeros_like(out)
     slack = torch.zeros(b, I, Hq, 1, dtype=torch.float64)
     for s in range(b):
+        lo, len_ = max(first[s], 0), min(max(lens[s], 0), n)
+        if len_ <= lo:
+            continue
+        seen = torch.arange(lo, len_) < (len_ - (I - 1 - torch.arange(I)))[:, None]      # (I, rows)
+        some = seen.any(1, keepdim=True)
         for h in range(Hq):
-            kk, vv = k[s, :, h // (Hq // Hkv)], v[s, :, h // (Hq // Hkv)]
-            for i in range(I):
-                lo, hi = max(first[s], 0), min(max(lens[s], 0), n) - (I - 1 - i)
-                if hi <= lo:
-                    continue
-                qq = q[s, i, h]
-                logit = kk[lo:hi] @ qq * scale
-                p = torch.softmax(logit, 0)
-                out[s, i, h] = p @ vv[lo:hi]
-                spread[s, i, h] = p @ vv[lo:hi].abs()
-                if dtype == torch.bfloat16:
-                    # A group's sum runs over 32 products u q (u <= 15) from -8 sum q: at most 40 additions of at most 23 sum |q|,
-                    # each off by a step of fp32, 2^-23; times the scale, an eighth of the group's largest |k| (1 + 2^-10).
-                    size = kk[lo:hi].abs().view(hi - lo, -1, GROUP).amax(-1) / 8 * (1 + 2 ** -10)
-                    err = (size @ qq.abs().view(-1, GROUP).sum(-1)) * 23 * 40 * 2.0 ** -23
-                    # up to four query rows of a cache are integers, each element off by half a step, 2^-15 of the row's largest
-                    if I * (Hq // Hkv) <= 4:
-                        err = err + kk[lo:hi].abs().sum(-1) * qq.abs().max() * 2.0 ** -14
-                    if blocks:   # every key may be off by half a step of fp16, and d products are added
-                        err = torch.maximum(err, (kk[lo:hi].abs() @ qq.abs()) * (2.0 ** -11 + d * 2.0 ** -23))
-                else:
-                    # 64 products (two halves of q, which leave 2^-22 of it out) from 0, then the groups
-                    err = (kk[lo:hi].abs() @ qq.abs()) * (72 * 2.0 ** -23 + 2.0 ** -22)
-                slack[s, i, h] = 2 * (err.max() * scale + logit.abs().max() * 8 * 2.0 ** -23)
+            kk, vv = k[s, lo:len_, h // (Hq // Hkv)], v[s, lo:len_, h // (Hq // Hkv)]
+            qq = q[s, :, h]
+            logit = qq @ kk.T * scale
+            p = torch.where(some, torch.softmax(torch.where(seen | ~some, logit, -math.inf), 1), 0.0)
+            out[s, :, h] = p @ vv
+            spread[s, :, h] = p @ vv.abs()
+            if dtype == torch.bfloat16:
+                # A group's sum runs over 32 products u q (u <= 15) from -8 sum q: at most 40 additions of at most 23 sum |q|,
+                # each off by a step of fp32, 2^-23; times the scale, an eighth of the group's largest |k| (1 + 2^-10).
+                size = kk.abs().view(len(kk), -1, GROUP).amax(-1) / 8 * (1 + 2 ** -10)
+                err = qq.abs().view(I, -1, GROUP).sum(-1) @ size.T * (23 * 40 * 2.0 ** -23)
+                # up to four query rows of a cache are integers, each element off by half a step, 2^-15 of the row's largest
+                if I * (Hq // Hkv) <= 4:
+                    err = err + kk.abs().sum(-1) * qq.abs().amax(-1, keepdim=True) * 2.0 ** -14
+                if blocks:   # every key may be off by half a step of fp16, and d products are added
+                    err = torch.maximum(err, qq.abs() @ kk.abs().T * (2.0 ** -11 + d * 2.0 ** -23))
+            else:
+                # 64 products (two halves of q, which leave 2^-22 of it out) from 0, then the groups
+                err = qq.abs() @ kk.abs().T * (72 * 2.0 ** -23 + 2.0 ** -22)
+            err = err * scale + logit.abs() * 8 * 2.0 ** -23
+            slack[s, :, h] = 2 * torch.where(seen, err, 0.0).amax(1, keepdim=True)
     return out, spread, slack
 
 

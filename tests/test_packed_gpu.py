@@ -228,41 +228,51 @@ def test_several_queries_are_causal(I, Hq, Hkv, dtype):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("I,Hq,Hkv", [(65, 1, 1), (128, 2, 2), (129, 1, 1), (256, 1, 1), (257, 2, 2), (40, 8, 2), (90, 6, 2), (300, 2, 1), (23, 12, 1)])
-def test_blocks_of_queries(I, Hq, Hkv, d):
+@pytest.mark.parametrize("b,I,Hq,Hkv,path", [(3, 65, 1, 1, 0), (40, 113, 2, 2, 1), (40, 128, 2, 2, 1), (40, 129, 2, 2, 1), (40, 256, 2, 2, 1),
+                                             (40, 257, 2, 2, 1), (40, 60, 4, 2, 1), (40, 40, 6, 2, 1), (40, 17, 24, 2, 1), (20, 300, 8, 4, 1),
+                                             (140, 8, 12, 1, 1), (2, 300, 8, 4, 0)])
+def test_blocks_of_queries(b, I, Hq, Hkv, path, d):
     n = 400
-    check_attend(3, Hq, Hkv, d, I, n, [n, I, 333], None, "bf16", seed=I)
-    check_attend(4, Hq, Hkv, d, I, n, [n - 1, I + 1, max(I - 3, 1), 0], [130, 0, 0, 5], "bf16", seed=I + 1)
+    for lens, first in (([n, I, 333], None), ([n - 1, I + 1, max(I - 3, 1), 0, 2 * I, 277], [130, 0, 0, 5, 128, 1])):
+        lens, first = [lens[s % len(lens)] for s in range(b)], first and [first[s % len(first)] for s in range(b)]
+        check_attend(b, Hq, Hkv, d, I, n, lens, first, "bf16", seed=I)
+        assert bm.last_packed_path() == path
 
 
 @pytest.mark.parametrize("spread", [1e-6, 1e-3, 100.0, 30000.0])
 def test_blocks_of_queries_over_values_of_any_size(spread):
-    check_attend(2, 2, 1, 128, 70, 200, [200, 77], None, "bf16", spread=spread, seed=31)
+    check_attend(64, 2, 2, 128, 70, 200, [200, 77] * 32, None, "bf16", spread=spread, seed=31)
+    assert bm.last_packed_path() == 1
 
 
 def test_blocks_over_long_caches():
     for d in (64, 128):
-        for expected in (0, 200):      # the length that a call expects decides which kernel takes it
-            check_attend(1, 2, 1, d, 70, 3000, [2999], [100], "bf16", seed=33, split=expected)
+        check_attend(1, 128, 128, d, 120, 3000, [2999], [100], "bf16", seed=33)
+        assert bm.last_packed_path() == 1
+        check_attend(1, 2, 1, d, 70, 3000, [2999], [100], "bf16", seed=34)
 
 
-def test_blocks_meet_rows_that_are_not_finite():
+@pytest.mark.parametrize("copies,path", [(1, 0), (20, 1)])
+def test_blocks_meet_rows_that_are_not_finite(copies, path):
     b, Hq, Hkv, d, I, n = 3, 2, 2, 128, 130, 300
     gen = torch.Generator().manual_seed(34)
     k, v, q = (rows(gen, b, t, h, d, dtype="bf16") for t, h in ((n, Hkv), (n, Hkv), (I, Hq)))
     v[0, 200, 0, 40] = math.nan                       # group 1, head 0: queries that see row 200
+    v[0, 260, 0, 41] = -math.inf                      # (a later one in the same group)
     k[1, 250, 1, 0] = math.inf                        # head 1: queries that see row 250
     k[2, 290:], v[2, 290:] = math.nan, math.inf       # behind sample 2's length
     k[2, :7], v[2, :7] = -math.inf, math.nan          # before its first row
     q[2, 5, 1, 3] = math.nan
-    cache = make(b, Hq, Hkv, d, n, "bf16", queries_max=I)
+    k, v, q = (t.repeat(copies, 1, 1, 1) for t in (k, v, q))
+    cache = make(b * copies, Hq, Hkv, d, n, "bf16", queries_max=I)
     cache.write(k, v)
-    out = cache.attend(q, ints([300, 300, 290]), first=ints([0, 0, 7])).float().cpu()
+    out = cache.attend(q, ints([300, 300, 290] * copies), first=ints([0, 0, 7] * copies)).float().cpu()
+    assert bm.last_packed_path() == path
     bad = torch.zeros(b, I, Hq, d, dtype=torch.bool)
     bad[0, I - 99 - 1:, 0, 32:64] = True              # query i sees rows below 300 - (129 - i): row 200 from i = 30 on
     bad[1, I - 49 - 1:, 1] = True
     bad[2, 5, 1] = True
-    assert torch.equal(out.isnan(), bad)
+    assert torch.equal(out.isnan(), bad.repeat(copies, 1, 1, 1))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -435,23 +445,24 @@ def test_a_captured_step_replayed_as_the_caches_grow():
 
 def test_a_captured_block_gives_what_an_eager_one_gives():
     gen = torch.Generator().manual_seed(35)
-    cache = make(2, 4, 2, 128, 600, "bf16", queries_max=150)
-    cache.write(rows(gen, 2, 600, 2, 128, dtype="bf16"), rows(gen, 2, 600, 2, 128, dtype="bf16"))
-    q, lens = rows(gen, 2, 150, 4, 128, dtype="bf16"), ints([600, 480])
+    cache = make(20, 4, 2, 128, 600, "bf16", queries_max=150)
+    cache.write(rows(gen, 20, 600, 2, 128, dtype="bf16"), rows(gen, 20, 600, 2, 128, dtype="bf16"))
+    q, lens = rows(gen, 20, 150, 4, 128, dtype="bf16"), ints([600, 480] * 10)
     want = cache.attend(q, lens)
+    assert bm.last_packed_path() == 1
     out = torch.zeros_like(q)
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         cache.attend(q, lens, out=out)
     for n in ([600, 480], [333, 600]):
-        lens.copy_(ints(n))
+        lens.copy_(ints(n * 10))
         graph.replay()
         assert torch.equal(out, want if n[0] == 600 else cache.attend(q, lens))
 
 
 def test_same_results_from_run_to_run():
     gen = torch.Generator().manual_seed(20)
-    for Hq, Hkv, I, n in ((32, 8, 1, 5000), (8, 8, 1, 700), (8, 2, 9, 300), (8, 2, 200, 500)):
+    for Hq, Hkv, I, n in ((32, 8, 1, 5000), (8, 8, 1, 700), (8, 2, 9, 300), (80, 40, 200, 500)):
         cache = make(2, Hq, Hkv, 128, n, "bf16", queries_max=I)
         cache.write(rows(gen, 2, n, Hkv, 128, dtype="bf16"), rows(gen, 2, n, Hkv, 128, dtype="bf16"))
         q, lens = rows(gen, 2, I, Hq, 128, dtype="bf16"), ints([n, n - 5])
