@@ -131,7 +131,7 @@ struct AttendArgs {
   int32_t query_tiles;    // of 8 (PAIR: 4) query rows, per cache
   int32_t runs;           // the most there may be: one for each warp of the grid
   int32_t slot_cols;      // query rows of a share in the workspace
-  FastDiv by_g, by_query_tiles;
+  FastDiv by_g, by_query_tiles, by_cols, by_heads;
   int32_t* before;        // workspace: [nsamples + 1] tiles (of one kv-head and query tile) of the samples before each
   float* partial;         // workspace: [runs][2][slot_cols][D + 4] sums of a cache's share, their maximum and sum of weights
 };
@@ -718,7 +718,7 @@ struct Joined {
   }
 };
 template <typename T, int D, int kGroups>
-__global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_combine_kernel(AttendArgs a, int cols_per_tile) {
+__global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_combine_kernel(AttendArgs a, int log_tile_cols) {
   constexpr int kPerRow = D / 4, kRows = kGroups == 1 ? 128 / kPerRow : 1, kBatch = 4;
   __shared__ float4 sums[kGroups][kPerRow];
   __shared__ float2 stats[kGroups];
@@ -728,11 +728,12 @@ __global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_c
   const int part = kGroups == 1 ? 0 : y;
   const int g = a.c.g, cols = a.I * g, at = x * 4;
   if (i >= (long long)a.c.nsamples * a.c.Hkv * cols) return;   // (uniform where kGroups > 1)
-  const int unit = (int)i / cols, col = (int)i % cols, qt = col / cols_per_tile, smp = unit / a.c.Hkv, head = unit % a.c.Hkv;
+  const int unit = a.by_cols((int)i), col = (int)i - unit * cols, qt = col >> log_tile_cols, smp = a.by_heads(unit), head = unit - smp * a.c.Hkv;
+  const int query = a.by_g(col);
   const long long per_sample = (long long)a.c.Hkv * a.query_tiles;
   const int before = a.before[smp], n = a.before[smp + 1] - before;
   const long long all = a.before[a.c.nsamples] * per_sample;
-  T* out = static_cast<T*>(a.out) + (((size_t)smp * a.I + col / g) * a.c.Hq + (size_t)head * g + col % g) * D + at;
+  T* out = static_cast<T*>(a.out) + (((size_t)smp * a.I + query) * a.c.Hq + (size_t)head * g + col - query * g) * D + at;
   if (n == 0) {
     if (part == 0) store4(out, 0.f, 0.f, 0.f, 0.f);
     return;
@@ -742,7 +743,7 @@ __global__ void __launch_bounds__(kGroups == 1 ? 128 : kGroups * D / 4) packed_c
   const int j0 = cut.of(begin), j1 = cut.of(begin + n - 1);
   if (j0 == j1) return;   // written out by its warp
   const size_t row = (size_t)a.slot_cols * (D + 4);
-  const float* p = a.partial + (size_t)(col - qt * cols_per_tile) * (D + 4);
+  const float* p = a.partial + (size_t)(col - (qt << log_tile_cols)) * (D + 4);
   Joined mine;
   for (int j = j0 + part; j <= j1; j += kBatch * kGroups) {
     float2 st[kBatch];
@@ -789,6 +790,8 @@ cudaError_t launch_columns(const AttendArgs& args, void* workspace, int max_len,
   a.slot_cols = (int)std::min<int64_t>(A::kCols, cols);
   a.by_g = FastDiv((uint32_t)a.c.g);
   a.by_query_tiles = FastDiv((uint32_t)a.query_tiles);
+  a.by_cols = FastDiv((uint32_t)cols);
+  a.by_heads = FastDiv((uint32_t)a.c.Hkv);
   a.before = static_cast<int32_t*>(workspace);
   a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + before_bytes(a.c.nsamples));
   static SmemConfigured configured;
@@ -798,17 +801,18 @@ cudaError_t launch_columns(const AttendArgs& args, void* workspace, int max_len,
   if (err != cudaSuccess) return err;
   const int64_t rows = units * cols;
   const int64_t shares = a.runs / (units * a.query_tiles);   // of a cache, more or less
-  const int cols_per_tile = (int)A::kCols;
+  constexpr int kLogCols = PAIR ? 2 : 3;
+  static_assert(1 << kLogCols == A::kCols, "");
   if (shares >= 32) {
     constexpr int kGroups = 4096 / D;   // 1024 threads
-    err = launch_dependent(packed_combine_kernel<T, D, kGroups>, dim3((unsigned)rows), dim3(1024), 0, st, a, cols_per_tile);
+    err = launch_dependent(packed_combine_kernel<T, D, kGroups>, dim3((unsigned)rows), dim3(1024), 0, st, a, kLogCols);
   } else if (shares >= 4) {
     constexpr int kGroups = 1024 / D;   // 256 threads
-    err = launch_dependent(packed_combine_kernel<T, D, kGroups>, dim3((unsigned)rows), dim3(256), 0, st, a, cols_per_tile);
+    err = launch_dependent(packed_combine_kernel<T, D, kGroups>, dim3((unsigned)rows), dim3(256), 0, st, a, kLogCols);
   } else {
     const int per_block = 128 / (D / 4);
     err = launch_dependent(packed_combine_kernel<T, D, 1>, dim3((unsigned)((rows + per_block - 1) / per_block)), dim3(128), 0, st, a,
-                           cols_per_tile);
+                           kLogCols);
   }
   count_launch();
   return err != cudaSuccess ? err : cudaGetLastError();
