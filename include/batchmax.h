@@ -369,7 +369,8 @@ bm_status_t bm_packed_write(bm_packed_t* cache, int32_t layer, int32_t sample0, 
 /* The same from the caches of an evicting handle: the n pairs of every cache of samples from_sample0 .. of from_layer, in storage order,
  * become rows 0 .. n - 1 (n: bm_cache_len; nothing happens where it is 0).  Both handles need the same dtype, head_dim, n_kv_heads and
  * device, else BM_ERR_INVALID; BM_ERR_STATE when the samples of the range hold different n or padding pairs; BM_ERR_CAPACITY when n is
- * above the packed capacity.  The pairs' positions and scores stay in the handle that is read. */
+ * above the packed capacity.  The pairs' positions and scores stay in the handle that is read, for which this is a call like its own: ordered
+ * on cuda_stream, and not to be made while another thread uses it. */
 bm_status_t bm_packed_write_from(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const bm_cache_t* from,
                                  int32_t from_layer, int32_t from_sample0, void* cuda_stream);
 
@@ -402,7 +403,8 @@ bm_status_t bm_packed_clear_status(bm_packed_t* cache, void* cuda_stream);
  * While enabled, every kernel launch of this library is bracketed by two CUDA events on its stream.
  * bm_profile_read waits for the recorded launches of one kernel class, returns their summed duration in
  * milliseconds and their count, and forgets them.  Not thread-safe; leave disabled in production. */
-enum { BM_KERNEL_ATTN_FWD = 0, BM_KERNEL_SCORE = 1, BM_KERNEL_EVICT = 2, BM_KERNEL_DECODE = 3 };
+enum { BM_KERNEL_ATTN_FWD = 0, BM_KERNEL_SCORE = 1, BM_KERNEL_EVICT = 2, BM_KERNEL_DECODE = 3,
+       BM_KERNEL_PACKED = 4 /* everything of packed caches */ };
 bm_status_t bm_profile_enable(int32_t on);
 bm_status_t bm_profile_read(int32_t kernel_class, float* total_ms /*HOST out*/, int32_t* launches /*HOST out*/);
 

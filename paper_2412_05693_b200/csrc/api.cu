@@ -147,7 +147,8 @@ struct bm_cache {
   static constexpr int kSlots = 4;
   Slot slots[kSlots];
   int next_slot = 0;
-  long dev_calls = 0, dev_calls_seen = -1;  // device-fed calls made / already ordered before the pipeline
+  mutable long dev_calls = 0;               // (packing a handle's caches reads them: such a call too)
+  long dev_calls_seen = -1;                 // device-fed calls made / already ordered before the pipeline
 };
 
 namespace {
@@ -238,6 +239,7 @@ int note_cuda_error(cudaError_t e) { return cuda_fail(e); }
 int cache_range_rows(const bm_cache* c, int layer, int sample0, int nsamples, CacheRows* out) {
   int n = 0, curr = 0;
   if (bm_status_t s = check_range(c, layer, sample0, nsamples, &n, &curr); s != BM_OK) return s;
+  ++c->dev_calls;  // a later host-fed call orders its pipeline after what reads the rows
   out->dtype = c->cfg.dtype; out->head_dim = c->cfg.head_dim; out->n_kv_heads = c->cfg.n_kv_heads; out->device = c->cfg.device;
   out->n = n;
   out->cap = c->cap;

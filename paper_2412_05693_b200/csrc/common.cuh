@@ -154,7 +154,7 @@ struct CacheRows {
 int cache_range_rows(const struct ::bm_cache* c, int layer, int sample0, int nsamples, CacheRows* out);   // a bm_status_t
 
 // Optional per-launch timing: when enabled, a ProfileScope brackets a launch with two CUDA events.
-enum KernelClass { kAttnFwd = 0, kScore = 1, kEvict = 2, kDecode = 3, kNumKernelClasses = 4 };
+enum KernelClass { kAttnFwd = 0, kScore = 1, kEvict = 2, kDecode = 3, kPacked = 4, kNumKernelClasses = 5 };
 void profile_begin(int cls, cudaStream_t st);
 void profile_end(int cls, cudaStream_t st);
 struct ProfileScope {

@@ -3,6 +3,10 @@
 // Both are bound by HBM: a row of d elements comes in as d * e bytes and goes out as d / 2 + d / 16, or the other way round.  A CTA has one
 // tile of a cache, whose bytes meet in shared memory, so that global memory sees whole 16-byte pieces although a tile's bytes are ordered for
 // the attention kernel.  A thread has eight consecutive elements of a row, four threads a group.
+//
+// Measured, 16 samples of 4096 rows, 8 heads, d = 128 (344 MB, 52.6 us at the copy bandwidth): bf16 written in 70 us, read in 56; d = 64 77 and
+// 57; fp32, half as many rows, 57 and 51 (46.8).  Reading is bound by HBM, writing bf16 by its instructions (16 per element's lane:
+// schedulers 84 % busy, the logic pipe 70 %); a CTA of 256 threads 77 and 61 (fp32 55 and 49).
 #include <algorithm>
 
 #include "packed.cuh"
@@ -281,6 +285,7 @@ cudaError_t write_t(const PackedView& c, const RowSource& src, int I, const int3
   const int tiles = start == nullptr ? (I + kPackedTile - 1) / kPackedTile : (I + 2 * kPackedTile - 2) / kPackedTile;   // that I rows may touch
   const long long blocks = (long long)c.nsamples * tiles * c.Hkv;
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  ProfileScope prof(kPacked, st);
   const cudaError_t err = launch_dependent(packed_write_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, src, I,
                                            FastDiv((uint32_t)c.Hkv), FastDiv((uint32_t)tiles), start, counts);
   count_launch();
@@ -292,6 +297,7 @@ cudaError_t read_t(const PackedView& c, int row0, int count, const int32_t* lens
   const int tiles = (row0 + count - 1) / kPackedTile - row0 / kPackedTile + 1;
   const long long blocks = (long long)c.nsamples * tiles * c.Hkv;
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+  ProfileScope prof(kPacked, st);
   const cudaError_t err = launch_dependent(packed_read_kernel<T, D>, dim3((unsigned)blocks), dim3(kThreads), 0, st, c, row0, count,
                                            FastDiv((uint32_t)c.Hkv), FastDiv((uint32_t)tiles), lens, static_cast<T*>(k_out), static_cast<T*>(v_out));
   count_launch();

@@ -182,6 +182,48 @@ def test_the_pairs_that_a_prefill_kept_are_packed(dtype, compaction):
     assert torch.equal(one.read(0, K, sample0=2)[0], gk[:1, :K]) and not one.read(0, K, nsamples=2)[0].any()
 
 
+def test_a_handle_fed_from_the_host_is_packed_between_its_calls():
+    """Host-fed calls run on the handle's own streams: those before a packing are read complete, those after wait for it."""
+    b, Hq, Hkv, d, K, I = 4, 8, 4, 128, 512, 512
+    gen = torch.Generator().manual_seed(40)
+    cfg = dict(batch=b, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=d, kv_max=K, block_max=I)
+    host = [[(torch.randn(b, I, h, d, generator=gen)).bfloat16().pin_memory() for h in (Hq, Hkv, Hkv)] for _ in range(4)]
+    want = []
+    for fed in (False, True):
+        handle, caches = bm.BatchMaxCache(bm.Config(**cfg)), [make(b, Hq, Hkv, d, K, "bf16") for _ in range(4)]
+        for i, (q, k, v) in enumerate(host):
+            if fed:
+                handle.prefill_block_host(q, k, v, i * I, torch.empty_like(q).pin_memory(), evict_to=K)
+            else:
+                handle.prefill_block(q.cuda(), k.cuda(), v.cuda(), i * I, evict_to=K)
+                torch.cuda.synchronize()
+            caches[i].write_from(handle)
+            if not fed:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        got = [torch.stack(c.read(0, K)) for c in caches]
+        if fed:
+            assert all(torch.equal(a, w) for a, w in zip(got, want))
+        want = got
+        handle.close()
+
+
+def test_kernels_of_packed_caches_are_timed():
+    cache = make(1, 2, 1, 64, 40, "bf16")
+    gen = torch.Generator().manual_seed(41)
+    k, q = rows(gen, 1, 40, 1, 64, dtype="bf16"), rows(gen, 1, 1, 2, 64, dtype="bf16")
+    lens = ints([40])
+
+    def calls():
+        cache.write(k, k)
+        cache.read(0, 40)
+        cache.attend(q, lens)
+
+    calls()
+    ms, launches = bm.binding.profile_pass(calls)["packed"]
+    assert launches == 4 and ms > 0 and "packed" not in bm.binding.profile_pass(lambda: None)
+
+
 # ---- attend -----------------------------------------------------------------------------------------------------------------
 def check_attend(b, Hq, Hkv, d, I, capacity, lens, first, dtype, seed=0, spread=1.0, scale=0.0, split=0, cache=None):
     blocks = dtype == "bf16" and I * (Hq // Hkv) > 64       # many query rows may go through fp16 tiles
