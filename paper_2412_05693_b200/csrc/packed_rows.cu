@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "packed.cuh"
+#include "tc_common.cuh"
 
 namespace bm {
 namespace {
@@ -102,8 +103,13 @@ __device__ __forceinline__ uint32_t quantise8(float* x, float s) {
     }
     constexpr float kStep = 192.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      m[i] = __float_as_uint(fminf(fmaf(x[i], inv, kStep), kStep + 7.f) + (kMagic - kStep + 8.f));
+    for (int i = 0; i < 8; i += 2) {
+      float t0, t1, k0, k1;
+      tc::fma2(t0, t1, x[i], x[i + 1], inv, kStep);
+      tc::add2g(k0, k1, fminf(t0, kStep + 7.f), fminf(t1, kStep + 7.f), kMagic - kStep + 8.f, kMagic - kStep + 8.f);
+      m[i] = __float_as_uint(k0);
+      m[i + 1] = __float_as_uint(k1);
+    }
   } else {
     // A quotient of 24 by 11 bits may be 2^-24 of itself away from a tie; x * inv errs by less than 2^-22 of itself.  Those within 2^-18 of a
     // half-integer are divided.
