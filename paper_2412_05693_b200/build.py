@@ -61,7 +61,7 @@ def build_fastcall(force: bool = False):
     part = f"{path}.{os.getpid()}"           # (another process may be importing the file, or building it too)
     try:
         subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", *("-I" + d for d in inc), "-o", part, FASTCALL_SRC,
-                        "-L" + os.path.join(torch_dir, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"], check=True)
+                        "-L" + os.path.join(torch_dir, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"], check=True)
         os.replace(part, path)
     finally:
         if os.path.exists(part):

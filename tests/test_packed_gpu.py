@@ -512,6 +512,79 @@ def test_same_results_from_run_to_run():
         assert all(torch.equal(cache.attend(q, lens), first) for _ in range(5))
 
 
+@pytest.mark.parametrize("b", [33, 64, 65, 1024, 2500])
+def test_many_samples_of_unequal_length(b):
+    """A warp finds its run among the samples' tiles: every lane has several samples, or more than fit one look."""
+    gen = torch.Generator().manual_seed(b)
+    lens = torch.randint(0, 71, (b,), generator=gen).tolist()
+    lens[3:9] = [0] * 6
+    check_attend(b, 2, 1, 64, 1, 70, lens, None, "bf16", seed=b)
+    check_attend(b, 1, 1, 64, 1, 70, [0] * (b - 1) + [70], None, "f32", seed=b)
+
+
+@pytest.mark.parametrize("b,Hq,I,path", [(3, 4, 1, 0), (40, 8, 64, 1)])
+def test_nothing_to_see(b, Hq, I, path):
+    cache = make(b, Hq, 2, 64, 200, "bf16", queries_max=I)
+    gen = torch.Generator().manual_seed(50)
+    cache.write(rows(gen, b, 200, 2, 64, dtype="bf16"), rows(gen, b, 200, 2, 64, dtype="bf16"))
+    q = rows(gen, b, I, Hq, 64, dtype="bf16")
+    for lens, first in (([0] * b, None), ([-3] * b, [5] * b), ([150] * b, [150] * b), ([200] * b, [2 ** 31 - 1] * b)):
+        out = torch.full_like(q, 7.0)
+        cache.attend(q, ints(lens), first=None if first is None else ints(first), out=out)
+        assert not out.any() and bm.last_packed_path() == path
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,I", [(4, 4, 64, 1), (8, 2, 128, 1), (8, 1, 64, 3)])
+def test_single_precision_has_all_its_digits(Hq, Hkv, d, I):
+    """The worst case that `bound` allows would hide a lost second half of a query or a weight (2^-12 of it, 1e-4 of the outputs): fp32
+    steps of logits up to 32 and of their sums leave a few 2^-20."""
+    gen = torch.Generator().manual_seed(55)
+    n = 900
+    k, v, q = (torch.randn(2, t, h, d, generator=gen).cuda() for t, h in ((n, Hkv), (n, Hkv), (I, Hq)))
+    cache = make(2, Hq, Hkv, d, n, "f32", queries_max=I)
+    cache.write(k, v)
+    out = cache.attend(q, ints([n, n - 100])).double().cpu()
+    want, _, _ = ref.attend(q.double().cpu(), ref.packed_values(k), ref.packed_values(v), [n, n - 100], [0, 0], d ** -0.5, torch.float32)
+    assert (out - want).norm() <= 2.0 ** -18 * want.norm()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [1e-3, 0.7, 6.0])
+def test_flat_and_peaked_weights(scale, dtype):
+    check_attend(2, 8, 2, 64, 1, 500, [500, 333], None, dtype, seed=51, scale=scale)
+    check_attend(2, 4, 2, 128, 2, 500, [500, 333], None, dtype, seed=52, scale=scale)
+
+
+def test_what_a_workspace_holds_before_does_not_matter():
+    gen = torch.Generator().manual_seed(53)
+    for b, Hq, Hkv, I in ((3, 8, 2, 1), (30, 8, 4, 64)):
+        cache = make(b, Hq, Hkv, 128, 700, "bf16", queries_max=I)
+        cache.write(rows(gen, b, 700, Hkv, 128, dtype="bf16"), rows(gen, b, 700, Hkv, 128, dtype="bf16"))
+        q, lens = rows(gen, b, I, Hq, 128, dtype="bf16"), ints([700, 0, 650] * (b // 3))
+        cache.workspace.zero_()
+        want = cache.attend(q, lens)
+        for byte in (0xff, 0x7f, 0x01):
+            cache.workspace.fill_(byte)
+            assert torch.equal(cache.attend(q, lens), want)
+
+
+def test_repeated_rows_counts_beyond_the_tokens_and_closed_caches():
+    gen = torch.Generator().manual_seed(54)
+    cache = make(3, 2, 2, 64, 70, "bf16")
+    k, v = rows(gen, 1, 40, 2, 64, dtype="bf16"), rows(gen, 3, 1, 2, 64, dtype="bf16")
+    cache.write(k.expand(3, -1, -1, -1), v.expand(-1, 40, -1, -1), start=ints([0, 30, 5]), counts=ints([1000, 40, -1]))
+    gk, gv = cache.read(0, 70)
+    wk, wv = ref.packed_values(k[0]), ref.packed_values(v)
+    same(gk[0, :40], wk)
+    same(gv[1, 30:], wv[1].expand(40, -1, -1))
+    assert not gk[0, 40:].any() and not gk[1, :30].any() and not gk[2].any() and cache.status() == 0
+    cache.close()
+    for call in (lambda: cache.read(0, 1), lambda: cache.write(v, v), lambda: cache.status()):
+        with pytest.raises(bm.BMError) as e:
+            call()
+        assert e.value.code == 1
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------------
 def test_prefill_with_eviction_then_decoding_over_packed_caches():
     """A prompt through an evicting handle, its kept pairs packed, tokens decoded over 4 bits."""
