@@ -1,7 +1,7 @@
 // Attention of blocks of queries over a packed cache (packed.cuh) on the 5th-generation tensor cores: what packed_attend.cu computes, for
 // calls whose query rows, I * g of a cache, fill tiles of 128.
 //
-// A CTA has two tiles of 128 query rows of one cache, A and B, and 128 keys at a time.  Four warps turn the packed rows into fp16 tiles in
+// A CTA has two tiles of 128 query rows of one cache, A and B, and 128 keys at a time.  Eight warps turn the packed rows into fp16 tiles in
 // shared memory (K as code * s, V likewise: 15 bits rounded to 11), one issues S = Q K^T of both, one each O += P V of A and of B, and
 // four softmax warps per tile have a thread for every query row, which also brought its row of Q.  Tensor memory: O_A | O_B | P_A | P_B | S
 // (one of 128 columns that the tiles use in turn at d = 128, one each at d = 64).  A group reads its row's 128 logits into registers at once
@@ -15,9 +15,11 @@
 // values are 0 in the tile, and the first such row of each group is kept: queries see a prefix of the rows, those that see it are NaN there.
 //
 // What bounds it: the softmax warps (exponentials 2048 cycles per pair of tiles, the tensor pipe as many) and, beside them on the same
-// schedulers, the unpacking (13 instructions for 8 elements, 430 per thread and 128 keys).  Measured, 256 queries of 4 samples over 4352
-// rows, 32 / 8 heads, d = 128: 103 us, 685 TFLOP/s (128 CTAs, 2.8 us per 128 keys; the tensor pipe busy 35 %), 16 samples 400; with the
-// unpacking left out 314; d = 64 76.  packed_scales_kernel 4.
+// schedulers, the unpacking (13 instructions for 8 elements, 230 per thread and 128 keys).  Measured, 256 queries of 4 samples over 4352
+// rows, 32 / 8 heads, d = 128: 93 us, 764 TFLOP/s (128 CTAs, 2.6 us per 128 keys), 16 samples of 4096 345, d = 64 75; one row tile, 32
+// queries of 16 samples of 4096, 69.  Four unpacking warps, with twice the work each (512 threads): 95, 370, 74,
+// 86; 64 keys per step with logits of its own for either row tile 98, 350, 87, 77; scales brought to range in pairs of fp16 92, 344, 76, 74;
+// masks of the rows at their load, which waits for it, 101 with four warps.  packed_scales_kernel 4.
 #include <algorithm>
 #include <cmath>
 
@@ -28,7 +30,7 @@ namespace bm {
 using namespace tc;
 namespace {
 
-constexpr int kRows = 128, kKeys = 128, kThreads = 512;
+constexpr int kRows = 128, kKeys = 128, kThreads = 640, kLaunchRegs = 96;
 constexpr int kScaleParts = 16;         // CTAs that look at a cache's scales
 constexpr float kRescale = 8.f;         // the maximum follows when logits pass it by this much (log2): weights stay below 2^8
 
@@ -126,7 +128,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a) {
   using S = BlockSmem<D>;
   using L = PackedLayout<D>;
-  constexpr int G = L::G, kQkWarp = 8, kPvWarp = 9 /* A; 10: B */, kUnpackWarp = 12;
+  constexpr int G = L::G, kQkWarp = 8, kPvWarp = 9 /* A; 10: B */, kUnpackWarp = 12, kUnpackWarps = 8;
   constexpr int NSB = D == 128 ? 1 : 2;   // logit buffers
   constexpr int B_Q = 0, B_KFULL = 2, B_KFREE = 4, B_VFULL = 6, B_VFREE = 8, B_SFULL = 10, B_SFREE = 12, B_P = 14 /* [half][group] */,
                 B_PV = 18 /* likewise */, B_COUNT = 22;
@@ -143,7 +145,10 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
     *abort_flag = 0;
 #pragma unroll 1
     for (int b = 0; b < B_COUNT; ++b)
-      mbar_init(&bars[b], b < B_KFREE || (b >= B_VFULL && b < B_VFREE) || (b >= B_SFREE && b < B_PV) ? 4 : b >= B_VFREE && b < B_SFULL ? 2 : 1);
+      mbar_init(&bars[b], b < B_KFULL || (b >= B_SFREE && b < B_PV) ? 4
+                          : b < B_KFREE || (b >= B_VFULL && b < B_VFREE) ? kUnpackWarps
+                          : b >= B_VFREE && b < B_SFULL                  ? 2
+                                                                         : 1);
     mbar_fence_init();
     for (int i = 0; i < 4; ++i) nan_row[i] = INT32_MAX;
   }
@@ -180,55 +185,45 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
   }
   auto pow2 = [](int e) { return __int_as_float((e + 127) << 23); };
 
+  // 640 threads start with kLaunchRegs = 96 registers each: 256 x 160 + 128 x 32 + 256 x 64
   if (warp >= kQkWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");   // 512 threads start with 128 registers each: 256 x 168 + 256 x 88
     if (warp >= kUnpackWarp) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
       // ------------------------------------------------------------------ packed rows -> fp16 tiles
-      const int d = tid - kUnpackWarp * 32;
+      const int u = tid - kUnpackWarp * 32, d = u & 127, half = u >> 7;
       const uint8_t* base = a.c.data + (size_t)unit * a.c.tiles * L::kBytes;
       const float fk = pow2(ek), fv = pow2(ev);
-      uint4 kc[D / 32], vc[2][2];   // this thread's codes: of key row d; of two pairs of value rows, 8 elements of each group
-      uint32_t ks[G / 2], vs[2][G];
-      // value task i: rows c and c + 4 of the tile's 8-row block (d + 128 i) / 16, the elements 8 rp .. + 7 of each group
+      // this thread's codes: of half of key row d; of the value rows vr and vr + 4, the elements 8 rp .. + 7 of each group
+      uint4 kc[D / 64], vc[2];
+      uint32_t ks[G / 2], vs[G];
+      const int rp = u / 4 % 4, vr = u / 16 * 8 + u % 4;
+      // Rows that no query sees are read as they are (of the last tile that has such rows, if theirs is behind it) and get scales of 0, when
+      // they are used: a mask at the load would wait for it.
+      const int last_tile = (seen.len - 1) / kPackedTile;
+      auto tile_at = [&](int row) { return base + (size_t)min(row / kPackedTile, last_tile) * L::kBytes; };
       auto load_keys = [&](int j) {
-        const int row = (t_first + j) * kKeys + d;
-        const bool in = row >= seen.lo && row < seen.len;
-        const uint8_t* tile = base + (size_t)(row / kPackedTile) * L::kBytes;
-        const int at = row % kPackedTile;
+        const uint8_t* tile = tile_at((t_first + j) * kKeys + d);
+        const int at = d % kPackedTile;
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) kc[i] = in ? ld_global_16(tile + at * (D / 2) + i * 16) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < D / 64; ++i) kc[i] = ld_global_16(tile + at * (D / 2) + (half * (D / 64) + i) * 16);
 #pragma unroll
-        for (int i = 0; i < G / 2; ++i) ks[i] = in ? *reinterpret_cast<const uint32_t*>(tile + L::kKeyScales + at * G * 2 + i * 4) : 0u;
+        for (int i = 0; i < G / 2; ++i) ks[i] = *reinterpret_cast<const uint32_t*>(tile + L::kKeyScales + at * G * 2 + i * 4);
       };
       auto load_values = [&](int j) {
-        const int row0 = (t_first + j) * kKeys;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int task = d + 128 * i, block = task / 16, rp = task / 4 % 4, c = task % 4, row = row0 + block * 8 + c;
-          const bool lo_in = row >= seen.lo && row < seen.len, hi_in = row + 4 >= seen.lo && row + 4 < seen.len;
-          const uint8_t* tile = base + (size_t)(row / kPackedTile) * L::kBytes;
-          const int at = row % kPackedTile;
-          const uint32_t keep = (lo_in ? 0x0000ffffu : 0u) | (hi_in ? 0xffff0000u : 0u);
-#pragma unroll
-          for (int g4 = 0; g4 < G; ++g4) vs[i][g4] = 0u;
-          vc[i][0] = vc[i][1] = make_uint4(0, 0, 0, 0);
-          if (keep != 0) {
-            if constexpr (G == 4) {
-              vc[i][0] = ld_global_16(tile + L::value_codes(at, 0, 2 * rp));
-              vc[i][1] = ld_global_16(tile + L::value_codes(at, 0, 2 * rp + 1));
-              const uint4 s = ld_global_16(tile + L::value_scale(at, 0));
-              vs[i][0] = s.x; vs[i][1] = s.y; vs[i][G - 2] = s.z; vs[i][G - 1] = s.w;
-            } else {
-              const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_codes(at, 0, 2 * rp));
-              const uint2 y = *reinterpret_cast<const uint2*>(tile + L::value_codes(at, 0, 2 * rp + 1));
-              vc[i][0] = make_uint4(x.x, x.y, 0, 0);
-              vc[i][1] = make_uint4(y.x, y.y, 0, 0);
-              const uint2 s = *reinterpret_cast<const uint2*>(tile + L::value_scale(at, 0));
-              vs[i][0] = s.x; vs[i][1] = s.y;
-            }
-#pragma unroll
-            for (int g4 = 0; g4 < G; ++g4) vs[i][g4] &= keep;
-          }
+        const uint8_t* tile = tile_at((t_first + j) * kKeys + vr);
+        const int at = vr % kPackedTile;
+        if constexpr (G == 4) {
+          vc[0] = ld_global_16(tile + L::value_codes(at, 0, 2 * rp));
+          vc[1] = ld_global_16(tile + L::value_codes(at, 0, 2 * rp + 1));
+          const uint4 s = ld_global_16(tile + L::value_scale(at, 0));
+          vs[0] = s.x; vs[1] = s.y; vs[G - 2] = s.z; vs[G - 1] = s.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(tile + L::value_codes(at, 0, 2 * rp));
+          const uint2 y = *reinterpret_cast<const uint2*>(tile + L::value_codes(at, 0, 2 * rp + 1));
+          vc[0] = make_uint4(x.x, x.y, 0, 0);
+          vc[1] = make_uint4(y.x, y.y, 0, 0);
+          const uint2 s = *reinterpret_cast<const uint2*>(tile + L::value_scale(at, 0));
+          vs[0] = s.x; vs[1] = s.y;
         }
       };
       if (T > 0) {
@@ -240,112 +235,126 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
         const int s = j & 1;
         if (j >= 2) wait(B_KFREE + s, j / 2 - 1);
         unsigned char* k = sm + S::kK + s * S::kTile;
+        const int row0 = (t_first + j) * kKeys;
+        auto seen_row = [&](int row) { return row >= seen.lo && row < seen.len; };
+        if (!seen_row(row0 + d)) {
+#pragma unroll
+          for (int i = 0; i < G / 2; ++i) ks[i] = 0u;
+        }
 #pragma unroll
         for (int g4 = 0; g4 < G; ++g4) {
           const float f = __half2float(__ushort_as_half((unsigned short)(ks[g4 / 2] >> (16 * (g4 % 2))))) * fk;
           const uint32_t s2 = half2_bits(f, f);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {   // the word (g4, c): word c G + g4 of the row
-            const int at = c * G + g4;
+          for (int i = 0; i < 2; ++i) {   // the word (g4, c): word c G + g4 of the row
+            const int c = 2 * half + i, at = i * G + g4;
             const uint4 four = kc[at / 4];
             const uint32_t w = at % 4 == 0 ? four.x : at % 4 == 1 ? four.y : at % 4 == 2 ? four.z : four.w;
             *reinterpret_cast<uint4*>(k + (4 * g4 + c) / 8 * 16384 + sw128_offset(d, (4 * g4 + c) % 8)) = unpack_scaled(w, s2);
           }
         }
-        if (j + 1 < T) load_keys(j + 1);   // (on its way while the values are unpacked, and theirs during the next keys)
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars[B_KFULL + s]);
+        if (j + 1 < T) load_keys(j + 1);   // (on its way while the values are unpacked, and theirs during the next keys)
         if (j >= 2) wait(B_VFREE + s, j / 2 - 1);
         unsigned char* v = sm + S::kV + s * S::kTile;
+        const uint32_t keep = (seen_row(row0 + vr) ? 0x0000ffffu : 0u) | (seen_row(row0 + vr + 4) ? 0xffff0000u : 0u);
+        uint32_t bad = 0;   // bit 15 of a half: some exponent is all ones
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int task = d + 128 * i, block = task / 16, rp = task / 4 % 4, c = task % 4;
+        for (int g4 = 0; g4 < G; ++g4) {
+          vs[g4] &= keep;
+          bad |= (vs[g4] & 0x7c007c00u) + 0x04000400u;
+        }
+        if (bad & 0x80008000u) {
 #pragma unroll
           for (int g4 = 0; g4 < G; ++g4) {
-            const uint32_t x = g4 == 0 ? vc[i][0].x : g4 == 1 ? vc[i][0].y : g4 == 2 ? vc[i][0].z : vc[i][0].w;
-            const uint32_t y = g4 == 0 ? vc[i][1].x : g4 == 1 ? vc[i][1].y : g4 == 2 ? vc[i][1].z : vc[i][1].w;
+            if (not_finite(vs[g4] >> 16)) { atomicMin(&nan_row[g4], row0 + vr + 4); vs[g4] &= 0x0000ffffu; }
+            if (not_finite(vs[g4])) { atomicMin(&nan_row[g4], row0 + vr); vs[g4] &= 0xffff0000u; }
+          }
+          __threadfence_block();
+        }
 #pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-              const uint32_t bits = vs[i][g4] >> (16 * hi) & 0xffffu;
-              float f = __half2float(__ushort_as_half((unsigned short)bits)) * fv;
-              if (not_finite(bits)) {
-                atomicMin(&nan_row[g4], (t_first + j) * kKeys + block * 8 + c + 4 * hi);
-                __threadfence_block();
-                f = 0.f;
-              }
-              const int piece = 4 * g4 + rp;
-              *reinterpret_cast<uint4*>(v + piece / 8 * 16384 + sw128_offset(block * 8 + c + 4 * hi, piece % 8)) =
-                  unpack_scaled(__byte_perm(x, y, hi ? 0x7632 : 0x5410), half2_bits(f, f));
-            }
+        for (int g4 = 0; g4 < G; ++g4) {
+          const uint32_t x = g4 == 0 ? vc[0].x : g4 == 1 ? vc[0].y : g4 == 2 ? vc[0].z : vc[0].w;
+          const uint32_t y = g4 == 0 ? vc[1].x : g4 == 1 ? vc[1].y : g4 == 2 ? vc[1].z : vc[1].w;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int hi = h ^ (rp & 1), piece = 4 * g4 + rp;   // (eight lanes write to all banks)
+            const float f = __half2float(__ushort_as_half((unsigned short)(vs[g4] >> (16 * hi)))) * fv;
+            *reinterpret_cast<uint4*>(v + piece / 8 * 16384 + sw128_offset(vr + 4 * hi, piece % 8)) =
+                unpack_scaled(__byte_perm(x, y, hi ? 0x7632 : 0x5410), half2_bits(f, f));
           }
         }
-        if (j + 1 < T) load_values(j + 1);
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars[B_VFULL + s]);
+        if (j + 1 < T) load_values(j + 1);
       }
-    } else if (lane == 0) {
-      const uint64_t dk_hi = smem_desc(0, 16, 1024) & 0xffffffff00000000ull;      // K-major operands (Q, K)
-      const uint32_t dk_lo = (uint32_t)(smem_desc(0, 16, 1024) & 0xffffffffull);
-      const uint64_t dv_hi = smem_desc(0, 16384, 1024) & 0xffffffff00000000ull;   // MN-major operand (V)
-      const uint32_t dv_lo = (uint32_t)(smem_desc(0, 16384, 1024) & 0xffffffffull);
-      constexpr uint32_t kBf16 = 1u << 7 | 1u << 10;                               // instr_desc's input formats: cleared, fp16
-      if (warp == kQkWarp) {
-        // ---------------------------------------------------------------- S = Q K^T of both tiles, in turn
-        const uint32_t idesc = instr_desc(kRows, kKeys, 0, 0) & ~kBf16;
-        const uint32_t q_lo = dk_lo + (smem_u32(sm + S::kQ) >> 4), k_base = dk_lo + (smem_u32(sm + S::kK) >> 4);
-        int sc0 = 0, sc1 = 0, last = -1;
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+      if (lane == 0) {
+        const uint64_t dk_hi = smem_desc(0, 16, 1024) & 0xffffffff00000000ull;      // K-major operands (Q, K)
+        const uint32_t dk_lo = (uint32_t)(smem_desc(0, 16, 1024) & 0xffffffffull);
+        const uint64_t dv_hi = smem_desc(0, 16384, 1024) & 0xffffffff00000000ull;   // MN-major operand (V)
+        const uint32_t dv_lo = (uint32_t)(smem_desc(0, 16384, 1024) & 0xffffffffull);
+        constexpr uint32_t kBf16 = 1u << 7 | 1u << 10;                               // instr_desc's input formats: cleared, fp16
+        if (warp == kQkWarp) {
+          // ---------------------------------------------------------------- S = Q K^T of both tiles, in turn
+          const uint32_t idesc = instr_desc(kRows, kKeys, 0, 0) & ~kBf16;
+          const uint32_t q_lo = dk_lo + (smem_u32(sm + S::kQ) >> 4), k_base = dk_lo + (smem_u32(sm + S::kK) >> 4);
+          int sc0 = 0, sc1 = 0, last = -1;
 #pragma unroll 1
-        for (int j = 0; j < T; ++j) {
-          wait(B_KFULL + (j & 1), j / 2);
-          const uint32_t k_lo = k_base + (uint32_t)(j & 1) * (S::kTile >> 4);
+          for (int j = 0; j < T; ++j) {
+            wait(B_KFULL + (j & 1), j / 2);
+            const uint32_t k_lo = k_base + (uint32_t)(j & 1) * (S::kTile >> 4);
 #pragma unroll 1
-          for (int x = 0; x < 2; ++x) {
-            if (j >= (x ? n1 : n0)) continue;
-            if (j == 0) wait(B_Q + x, 0);
-            const int before = NSB == 2 ? x : last, n = before == 0 ? sc0 : sc1;   // the logits that the buffer holds have been read
-            if (before >= 0 && n > 0) wait(B_SFREE + before, n - 1);
-            last = x;
-            if (x == 0) ++sc0; else ++sc1;
-            tc_fence_after();
-            const uint32_t q = q_lo + x * (S::kTile >> 4);
+            for (int x = 0; x < 2; ++x) {
+              if (j >= (x ? n1 : n0)) continue;
+              if (j == 0) wait(B_Q + x, 0);
+              const int before = NSB == 2 ? x : last, n = before == 0 ? sc0 : sc1;   // the logits that the buffer holds have been read
+              if (before >= 0 && n > 0) wait(B_SFREE + before, n - 1);
+              last = x;
+              if (x == 0) ++sc0; else ++sc1;
+              tc_fence_after();
+              const uint32_t q = q_lo + x * (S::kTile >> 4);
 #pragma unroll
-            for (int step = 0; step < D / 16; ++step) {
-              const uint32_t off = (step >> 2) * 1024 + (step & 3) * 2;   // (piece * 16384 + step * 32) / 16
-              mma_ss(tm_s0 + (NSB == 2 ? 128 * x : 0), dk_hi | (q + off), dk_hi | (k_lo + off), idesc, step > 0 ? 1u : 0u);
+              for (int step = 0; step < D / 16; ++step) {
+                const uint32_t off = (step >> 2) * 1024 + (step & 3) * 2;   // (piece * 16384 + step * 32) / 16
+                mma_ss(tm_s0 + (NSB == 2 ? 128 * x : 0), dk_hi | (q + off), dk_hi | (k_lo + off), idesc, step > 0 ? 1u : 0u);
+              }
+              mma_commit(&bars[B_SFULL + x]);
             }
-            mma_commit(&bars[B_SFULL + x]);
+            mma_commit(&bars[B_KFREE + (j & 1)]);
           }
-          mma_commit(&bars[B_KFREE + (j & 1)]);
-        }
-      } else if (warp == kPvWarp || warp == kPvWarp + 1) {
-        // ---------------------------------------------------------------- O += P V of tile x, 64 keys at a time
-        const int x = warp - kPvWarp, n = x ? n1 : n0;
-        const uint32_t idesc = instr_desc(kRows, D, 0, 1) & ~kBf16;   // V is MN-major: d contiguous, keys along K
-        const uint32_t v_base = dv_lo + (smem_u32(sm + S::kV) >> 4);
-        const uint32_t tm_o = tm_o0 + D * x, tm_p = tm_p0 + 64 * x;
+        } else if (warp == kPvWarp || warp == kPvWarp + 1) {
+          // ---------------------------------------------------------------- O += P V of tile x, 64 keys at a time
+          const int x = warp - kPvWarp, n = x ? n1 : n0;
+          const uint32_t idesc = instr_desc(kRows, D, 0, 1) & ~kBf16;   // V is MN-major: d contiguous, keys along K
+          const uint32_t v_base = dv_lo + (smem_u32(sm + S::kV) >> 4);
+          const uint32_t tm_o = tm_o0 + D * x, tm_p = tm_p0 + 64 * x;
 #pragma unroll 1
-        for (int j = 0; j < T; ++j) {
-          wait(B_VFULL + (j & 1), j / 2);
-          if (j >= n) { mbar_arrive(&bars[B_VFREE + (j & 1)]); continue; }
-          const uint32_t v_lo = v_base + (uint32_t)(j & 1) * (S::kTile >> 4);
+          for (int j = 0; j < T; ++j) {
+            wait(B_VFULL + (j & 1), j / 2);
+            if (j >= n) { mbar_arrive(&bars[B_VFREE + (j & 1)]); continue; }
+            const uint32_t v_lo = v_base + (uint32_t)(j & 1) * (S::kTile >> 4);
 #pragma unroll 1
-          for (int h = 0; h < 2; ++h) {
-            wait(B_P + 2 * h + x, j);
-            tc_fence_after();
+            for (int h = 0; h < 2; ++h) {
+              wait(B_P + 2 * h + x, j);
+              tc_fence_after();
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              mma_ts(tm_o, tm_p + (4 * h + q) * 8, dv_hi | (v_lo + (4 * h + q) * 128), idesc, j > 0 || h > 0 || q > 0 ? 1u : 0u);
-            mma_commit(&bars[B_PV + 2 * h + x]);
+              for (int q = 0; q < 4; ++q)
+                mma_ts(tm_o, tm_p + (4 * h + q) * 8, dv_hi | (v_lo + (4 * h + q) * 128), idesc, j > 0 || h > 0 || q > 0 ? 1u : 0u);
+              mma_commit(&bars[B_PV + 2 * h + x]);
+            }
+            mma_commit(&bars[B_VFREE + (j & 1)]);
           }
-          mma_commit(&bars[B_VFREE + (j & 1)]);
         }
       }
     }
   } else {
     // -------------------------------------------------------------------- a thread per query row
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
     const int x = warp >> 2, quad = warp & 3, r = quad * 32 + lane, n = x ? n1 : n0;
     const int col = (2 * pair + x) * kRows + r, query = a.by_g(min(col, cols - 1)), in_group = min(col, cols - 1) - query * a.c.g;
     const uint32_t lane_addr = (uint32_t)(quad * 32) << 16;
@@ -379,13 +388,15 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars[B_Q + x]);
     }
+    // tiles that every row of the warp sees whole
+    const int full0 = seen.lo % kKeys ? 1 : 0, full1 = (__reduce_min_sync(0xffffffffu, limit) - t_first * kKeys) >> 7;
     float m_used = -INFINITY, l = 0.f;
 #pragma unroll 1
     for (int j = 0; j < n; ++j) {
       wait(B_SFULL + x, j);
       tc_fence_after();
       const int row0 = (t_first + j) * kKeys, v0 = max(seen.lo - row0, 0), v1 = min(limit - row0, kKeys);   // visible columns [v0, v1)
-      if (!__all_sync(0xffffffffu, v0 == 0 && v1 == kKeys)) {
+      if (j < full0 || j >= full1) {
         // hidden logits become -inf, in tensor memory and in a rolled loop: these tiles are few
 #pragma unroll 1
         for (int cc = 0; cc < 8; ++cc) {
@@ -507,6 +518,12 @@ cudaError_t launch_d(const PackedView& c, const PackedAttend& p, cudaStream_t st
   if (units * std::max<int64_t>(a.pairs, kScaleParts) > 0x7fffffff) return cudaErrorInvalidConfiguration;
   static SmemConfigured configured;
   if (cudaError_t err = configured.ensure(packed_block_kernel<D>, BlockSmem<D>::kTotal); err != cudaSuccess) return err;
+  // its warps divide the registers among them anew: with fewer at the launch than that takes they would wait for good
+  static const bool enough = [] {
+    cudaFuncAttributes attr;
+    return cudaFuncGetAttributes(&attr, packed_block_kernel<D>) == cudaSuccess && attr.numRegs >= kLaunchRegs;
+  }();
+  if (!enough) return cudaErrorInvalidConfiguration;
   cudaError_t err;
   {
     ProfileScope prof(kPacked, st);
@@ -522,15 +539,18 @@ cudaError_t launch_d(const PackedView& c, const PackedAttend& p, cudaStream_t st
 
 }  // namespace
 
-// Which calls take this kernel: its time goes by rounds of one CTA per SM and 128 keys, that of the warps' kernel by tiles of 32 keys x 8
-// query rows, shared evenly.  us, this kernel / the other: 32 / 8 heads, d = 128, 16 samples of 4096 rows, 32 query rows of a cache 100 /
-// 61, 64 rows 100 / 110, 128 rows 102 / 212; 4 samples, 64 rows 86 / 42, 128 rows 86 / 60, 256 rows 97 / 110, 1024 rows (4352) 103 / 432;
-// 1 sample of 4352, 256 rows 97 / 43, 1024 rows 98 / 115; of 16384, 512 rows 336 / 204; 64 samples of 1024, 64 rows 119 / 125; 32 samples of
-// 2048, 32 heads without groups, 64 rows 390 / 433; 8 kv-heads, d = 64, 4 samples of 4352, 1024 rows 76 / 264.
+// Which calls take this kernel: its time goes by rounds of one CTA per SM, 5 us and so much for 128 keys of one or of two row tiles; that of
+// the warps' kernel by tiles of 32 keys x 8 query rows, shared evenly, and 5 us.  us, this kernel / the other: 32 / 8 heads, d = 128, 16 samples of
+// 4096 rows, 32 query rows of a cache 67 / 60, 64 rows 68 / 110, 128 rows 69 / 211; 4 samples, 64 rows 64 / 40, 128 rows 65 / 60, 256 rows
+// 86 / 109, 1024 rows (4352) 93 / 429; 1 sample of 4352, 256 rows 90 / 41, 1024 rows 90 / 114; of 16384, 512 rows 305 / 203; 64 samples of
+// 1024, 32 rows 92 / 67, 64 rows 95 / 122; 32 samples of 2048, 32 heads without groups, 32 rows 269 / 239, 64 rows 273 / 425.  8 kv-heads,
+// d = 64, 16 samples of 4096, 32 rows 58 / 43, 64 rows 58 / 73; 4 of 4352, 256 rows 74 / 72, 512 rows 74 / 136; 1, 1024 rows 73 / 70;
+// short caches: 128 samples of 256, d = 128, 64 rows 94 / 86, 128 rows 104 / 162; 40 samples of 400 with 2 heads, d = 64, 257 rows 29 / 28.
 bool packed_block_pays(int d, const PackedView& c, int I, int max_len) {
   const double cols = (double)I * c.g, units = (double)c.nsamples * c.Hkv, pairs = std::ceil(cols / (2 * kRows));
-  const double here = (d == 64 ? 2.1 : 2.75) * std::ceil(units * pairs / sm_count()) * max_len / kKeys;
-  const double warps = (d == 64 ? 0.81 : 1.36) * units * std::ceil(cols / 8) * max_len / kPackedTile / (12. * sm_count());
+  const double step = d == 64 ? (cols <= kRows ? 1.7 : 2.08) : (cols <= kRows ? 2. : 2.57);
+  const double here = (5. + step * max_len / kKeys) * std::ceil(units * pairs / sm_count());
+  const double warps = 5. + (d == 64 ? 0.81 : 1.36) * units * std::ceil(cols / 8) * max_len / kPackedTile / (12. * sm_count());
   return here < warps;
 }
 

@@ -271,7 +271,7 @@ def test_several_queries_are_causal(I, Hq, Hkv, dtype):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("b,I,Hq,Hkv,path", [(3, 65, 1, 1, 0), (40, 113, 2, 2, 1), (40, 128, 2, 2, 1), (40, 129, 2, 2, 1), (40, 256, 2, 2, 1),
-                                             (40, 257, 2, 2, 1), (40, 60, 4, 2, 1), (40, 40, 6, 2, 1), (40, 17, 24, 2, 1), (20, 300, 8, 4, 1),
+                                             (60, 257, 2, 2, 1), (40, 60, 4, 2, 1), (40, 40, 6, 2, 1), (40, 17, 24, 2, 1), (20, 300, 8, 4, 1),
                                              (140, 8, 12, 1, 1), (2, 300, 8, 4, 0)])
 def test_blocks_of_queries(b, I, Hq, Hkv, path, d):
     n = 400
