@@ -14,12 +14,13 @@
 // A scale that is not finite: keys give NaN logits.  A weight of 0 times a NaN value would be NaN for queries that do not see the row, so such
 // values are 0 in the tile, and the first such row of each group is kept: queries see a prefix of the rows, those that see it are NaN there.
 //
-// What bounds it: the softmax warps (exponentials 2048 cycles per pair of tiles, the tensor pipe as many) and, beside them on the same
-// schedulers, the unpacking (13 instructions for 8 elements, 230 per thread and 128 keys).  Measured, 256 queries of 4 samples over 4352
-// rows, 32 / 8 heads, d = 128: 93 us, 764 TFLOP/s (128 CTAs, 2.6 us per 128 keys), 16 samples of 4096 345, d = 64 75; one row tile, 32
-// queries of 16 samples of 4096, 69.  Four unpacking warps, with twice the work each (512 threads): 95, 370, 74,
-// 86; 64 keys per step with logits of its own for either row tile 98, 350, 87, 77; scales brought to range in pairs of fp16 92, 344, 76, 74;
-// masks of the rows at their load, which waits for it, 101 with four warps.  packed_scales_kernel 4.
+// What bounds it: issue slots and latency of the softmax warps (exponentials 2048 cycles per pair of tiles and scheduler, the tensor pipe as
+// many, of 4400) and, beside them on the same schedulers, the unpacking (a third of the instructions).  Measured, 256 queries of 4 samples
+// over 4352 rows, 32 / 8 heads, d = 128: 89 us, 794 TFLOP/s (128 CTAs, 2.5 us per 128 keys), 16 samples of 4096 332, d = 64 75; one row
+// tile, 32 queries of 16 samples of 4096, 66.  With addresses and scales worked out per element group 93, 345, 75, 69; four unpacking warps
+// with twice the work each (512 threads) 95, 370, 74, 86; those with a mask at the rows' load, which waits for it, 101, 392, 77, 93.
+// 64 keys per step, with logits of its own for either row tile, took 98, 350, 87, 77 where 128 took 94, 349, 74, 69: a step's waits and
+// reductions come twice.  packed_scales_kernel 4.
 #include <algorithm>
 #include <cmath>
 
@@ -180,8 +181,8 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
 #pragma unroll
     for (int i = 0; i < kScaleParts; ++i) { mk = max(mk, p[2 * i]); mv = max(mv, p[2 * i + 1]); }
     const float fk = __half2float(__ushort_as_half((unsigned short)mk)), fv = __half2float(__ushort_as_half((unsigned short)mv));
-    if (mk > 0) ek = 11 - ((int)(__float_as_uint(fk) >> 23) - 127);
-    if (mv > 0) ev = 11 - ((int)(__float_as_uint(fv) >> 23) - 127);   // -4 .. 35
+    if (mk > 0) ek = min(11 - ((int)(__float_as_uint(fk) >> 23) - 127), 30);
+    if (mv > 0) ev = min(11 - ((int)(__float_as_uint(fv) >> 23) - 127), 30);   // -4 .. 30
   }
   auto pow2 = [](int e) { return __int_as_float((e + 127) << 23); };
 
@@ -192,11 +193,16 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
       // ------------------------------------------------------------------ packed rows -> fp16 tiles
       const int u = tid - kUnpackWarp * 32, d = u & 127, half = u >> 7;
       const uint8_t* base = a.c.data + (size_t)unit * a.c.tiles * L::kBytes;
-      const float fk = pow2(ek), fv = pow2(ev);
+      auto power = [&](int e) { return half2_bits(pow2(e), pow2(e)); };
+      const uint32_t k1 = power(min(ek, 15)), k2 = power(max(ek - 15, 0)), v1 = power(min(ev, 15)), v2 = power(max(ev - 15, 0));
       // this thread's codes: of half of key row d; of the value rows vr and vr + 4, the elements 8 rp .. + 7 of each group
       uint4 kc[D / 64], vc[2];
       uint32_t ks[G / 2], vs[G];
       const int rp = u / 4 % 4, vr = u / 16 * 8 + u % 4;
+      // where they go, in the tile: key row d's pieces 2 half, the others by flipping bits; the pieces rp of the value rows, the odd rp
+      // the later row first (eight lanes write to all banks)
+      const uint32_t k_at = S::kK + sw128_offset(d, 2 * half), v_at = S::kV + sw128_offset(vr + 4 * (rp & 1), rp);
+      const uint32_t first_half = rp & 1 ? 0x7632 : 0x5410, first_scale = rp & 1 ? 0x3232 : 0x1010;
       // Rows that no query sees are read as they are (of the last tile that has such rows, if theirs is behind it) and get scales of 0, when
       // they are used: a mask at the load would wait for it.
       const int last_tile = (seen.len - 1) / kPackedTile;
@@ -234,7 +240,6 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
       for (int j = 0; j < T; ++j) {
         const int s = j & 1;
         if (j >= 2) wait(B_KFREE + s, j / 2 - 1);
-        unsigned char* k = sm + S::kK + s * S::kTile;
         const int row0 = (t_first + j) * kKeys;
         auto seen_row = [&](int row) { return row >= seen.lo && row < seen.len; };
         if (!seen_row(row0 + d)) {
@@ -242,15 +247,16 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
           for (int i = 0; i < G / 2; ++i) ks[i] = 0u;
         }
 #pragma unroll
+        for (int i = 0; i < G / 2; ++i) ks[i] = hmul2(hmul2(ks[i], k1), k2);
+#pragma unroll
         for (int g4 = 0; g4 < G; ++g4) {
-          const float f = __half2float(__ushort_as_half((unsigned short)(ks[g4 / 2] >> (16 * (g4 % 2))))) * fk;
-          const uint32_t s2 = half2_bits(f, f);
+          const uint32_t s2 = __byte_perm(ks[g4 / 2], 0, g4 % 2 ? 0x3232 : 0x1010);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {   // the word (g4, c): word c G + g4 of the row
-            const int c = 2 * half + i, at = i * G + g4;
+            const int at = i * G + g4;
             const uint4 four = kc[at / 4];
             const uint32_t w = at % 4 == 0 ? four.x : at % 4 == 1 ? four.y : at % 4 == 2 ? four.z : four.w;
-            *reinterpret_cast<uint4*>(k + (4 * g4 + c) / 8 * 16384 + sw128_offset(d, (4 * g4 + c) % 8)) = unpack_scaled(w, s2);
+            *reinterpret_cast<uint4*>(sm + ((k_at + s * S::kTile) ^ (4 * (g4 % 2) + i) << 4) + g4 / 2 * 16384) = unpack_scaled(w, s2);
           }
         }
         fence_async_smem();
@@ -258,7 +264,6 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
         if (lane == 0) mbar_arrive(&bars[B_KFULL + s]);
         if (j + 1 < T) load_keys(j + 1);   // (on its way while the values are unpacked, and theirs during the next keys)
         if (j >= 2) wait(B_VFREE + s, j / 2 - 1);
-        unsigned char* v = sm + S::kV + s * S::kTile;
         const uint32_t keep = (seen_row(row0 + vr) ? 0x0000ffffu : 0u) | (seen_row(row0 + vr + 4) ? 0xffff0000u : 0u);
         uint32_t bad = 0;   // bit 15 of a half: some exponent is all ones
 #pragma unroll
@@ -276,14 +281,14 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
         }
 #pragma unroll
         for (int g4 = 0; g4 < G; ++g4) {
+          vs[g4] = hmul2(hmul2(vs[g4], v1), v2);
           const uint32_t x = g4 == 0 ? vc[0].x : g4 == 1 ? vc[0].y : g4 == 2 ? vc[0].z : vc[0].w;
           const uint32_t y = g4 == 0 ? vc[1].x : g4 == 1 ? vc[1].y : g4 == 2 ? vc[1].z : vc[1].w;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int hi = h ^ (rp & 1), piece = 4 * g4 + rp;   // (eight lanes write to all banks)
-            const float f = __half2float(__ushort_as_half((unsigned short)(vs[g4] >> (16 * hi)))) * fv;
-            *reinterpret_cast<uint4*>(v + piece / 8 * 16384 + sw128_offset(vr + 4 * hi, piece % 8)) =
-                unpack_scaled(__byte_perm(x, y, hi ? 0x7632 : 0x5410), half2_bits(f, f));
+            const uint32_t words = h == 0 ? first_half : first_half ^ 0x2222;
+            *reinterpret_cast<uint4*>(sm + ((v_at + s * S::kTile) ^ (h ^ g4 % 2) << 6 ^ h << 9) + g4 / 2 * 16384) =
+                unpack_scaled(__byte_perm(x, y, words), __byte_perm(vs[g4], 0, h == 0 ? first_scale : first_scale ^ 0x2222));
           }
         }
         fence_async_smem();
@@ -540,15 +545,16 @@ cudaError_t launch_d(const PackedView& c, const PackedAttend& p, cudaStream_t st
 }  // namespace
 
 // Which calls take this kernel: its time goes by rounds of one CTA per SM, 5 us and so much for 128 keys of one or of two row tiles; that of
-// the warps' kernel by tiles of 32 keys x 8 query rows, shared evenly, and 5 us.  us, this kernel / the other: 32 / 8 heads, d = 128, 16 samples of
-// 4096 rows, 32 query rows of a cache 67 / 60, 64 rows 68 / 110, 128 rows 69 / 211; 4 samples, 64 rows 64 / 40, 128 rows 65 / 60, 256 rows
-// 86 / 109, 1024 rows (4352) 93 / 429; 1 sample of 4352, 256 rows 90 / 41, 1024 rows 90 / 114; of 16384, 512 rows 305 / 203; 64 samples of
-// 1024, 32 rows 92 / 67, 64 rows 95 / 122; 32 samples of 2048, 32 heads without groups, 32 rows 269 / 239, 64 rows 273 / 425.  8 kv-heads,
-// d = 64, 16 samples of 4096, 32 rows 58 / 43, 64 rows 58 / 73; 4 of 4352, 256 rows 74 / 72, 512 rows 74 / 136; 1, 1024 rows 73 / 70;
-// short caches: 128 samples of 256, d = 128, 64 rows 94 / 86, 128 rows 104 / 162; 40 samples of 400 with 2 heads, d = 64, 257 rows 29 / 28.
+// the warps' kernel by tiles of 32 keys x 8 query rows, shared evenly, and 5 us.  us, this kernel / the other: 32 / 8 heads, d = 128, 16
+// samples of 4096 rows, 32 query rows of a cache 64 / 60, 64 rows 65 / 110, 128 rows 66 / 211; 4 samples, 64 rows 62 / 40, 128 rows 63 / 60,
+// 256 rows 83 / 109, 1024 rows (4352) 89 / 429; 1 sample of 4352, 256 rows 86 / 41, 1024 rows 87 / 114; of 16384, 512 rows 289 / 203; 64
+// samples of 1024, 32 rows 91 / 67, 64 rows 93 / 122; 32 samples of 2048, 32 heads without groups, 32 rows 255 / 239, 64 rows 260 / 425.
+// 8 kv-heads, d = 64, 16 samples of 4096, 32 rows 58 / 43, 64 rows 58 / 73; 4 of 4352, 256 rows 73 / 72, 512 rows 74 / 136; 1, 1024 rows
+// 73 / 70; short caches: 128 samples of 256, d = 128, 64 rows 94 / 86, 128 rows 103 / 162; 40 samples of 400 with 2 heads, d = 64, 257
+// rows 29 / 28.
 bool packed_block_pays(int d, const PackedView& c, int I, int max_len) {
   const double cols = (double)I * c.g, units = (double)c.nsamples * c.Hkv, pairs = std::ceil(cols / (2 * kRows));
-  const double step = d == 64 ? (cols <= kRows ? 1.7 : 2.08) : (cols <= kRows ? 2. : 2.57);
+  const double step = d == 64 ? (cols <= kRows ? 1.7 : 2.08) : (cols <= kRows ? 1.9 : 2.45);
   const double here = (5. + step * max_len / kKeys) * std::ceil(units * pairs / sm_count());
   const double warps = 5. + (d == 64 ? 0.81 : 1.36) * units * std::ceil(cols / 8) * max_len / kPackedTile / (12. * sm_count());
   return here < warps;
