@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kThreads) packed_read_kernel(PackedView c, int
   const int rest = by_heads(blockIdx.x), head = blockIdx.x - rest * c.Hkv, smp = by_tiles(rest);
   const int t = row0 / kPackedTile + rest - smp * (int)by_tiles.d, base = t * kPackedTile;
   const int first = max(row0 - base, 0), last = min(row0 + count - base, kPackedTile);   // rows of the tile, [first, last)
-  const int len = lens != nullptr ? min(max(lens[smp] - base, 0), kPackedTile) : kPackedTile;
+  const int len = lens != nullptr ? min(max(lens[smp], 0), c.capacity) - base : kPackedTile;   // rows of the tile below the sample's length
   const uint8_t* tile = c.data + (((size_t)smp * c.Hkv + head) * c.tiles + t) * L::kBytes;
   for (int i = threadIdx.x; i < L::kBytes / 16; i += kThreads) {
     // pieces of key codes are of one row, those of value codes of eight

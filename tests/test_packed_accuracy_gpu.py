@@ -1,0 +1,48 @@
+"""Packed caches: what outputs owe to the rows that a query sees, and to nothing else, against 64 bits on the GPU.
+
+An output of bf16 is a number near the exact one, rounded: its rounding alone is 2^-8 / sqrt(3) of it at most in the mean square
+(an error even over a step that is 2^-7 of the power of two below the value), 2.26e-3.  Where weights go through fp16, once or twice,
+each adds 2^-11 / sqrt(3) of the value at most, 2.8e-4, independent from row to row.  Together 2.3e-3: DIGITS allows 2.5e-3.
+"""
+import pytest
+import torch
+
+import paper_2412_05693_b200 as bm
+from tests import packed_reference as ref
+from tests.test_packed_gpu import DT, ints, make, same
+
+pytestmark = pytest.mark.gpu
+DIGITS = 2.5e-3
+
+
+def exact(q, k, v, lens, first, scale):
+    """The attention in 64 bits over what k and v are packed as; q (b, I, Hq, d), k and v (b, n, Hkv, d)."""
+    b, I, Hq, d = q.shape
+    n, Hkv = k.shape[1:3]
+    k, v = (ref.packed_values(x).cuda().repeat_interleave(Hq // Hkv, 2) for x in (k, v))
+    row, query = torch.arange(n, device="cuda"), torch.arange(I, device="cuda")
+    seen = (row < (ints(lens)[:, None] - (I - 1 - query))[..., None]) & (row >= ints(first)[:, None, None])
+    k, v = (torch.where(seen.any(1)[..., None, None], x, 0.0) for x in (k, v))
+    logits = torch.einsum("bihd,bnhd->bhin", q.double(), k) * scale
+    seen = seen[:, None].expand_as(logits)
+    p = torch.where(seen.any(-1, keepdim=True), logits.masked_fill(~seen, -torch.inf).softmax(-1), 0.0)
+    return torch.einsum("bhin,bnhd->bihd", p, v)
+
+
+def normal(gen, *shape):
+    return torch.randn(*shape, generator=gen, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_far_below_zero_read_as_zeros(dtype):
+    gen = torch.Generator("cuda").manual_seed(1)
+    lens = [-2 ** 31, -2 ** 31 + 40, -1, 2 ** 31 - 1, 50]
+    cache = make(5, 2, 2, 64, 100, dtype)
+    k = normal(gen, 5, 100, 2, 64).to(DT[dtype])
+    cache.write(k, -k)
+    for row0, rows in ((0, 100), (40, 60), (65, 35), (99, 1)):
+        for got, x in zip(cache.read(row0, rows, lens=ints(lens)), (k, -k)):
+            want = ref.packed_values(x)[:, row0:row0 + rows]
+            want[:3] = 0
+            want[4, max(0, 50 - row0):] = 0
+            same(got, want)
