@@ -59,7 +59,7 @@ __device__ __forceinline__ Seen seen_rows(const BlockArgs16& a, int smp) {
   return s;
 }
 
-// The largest scales of a cache, in kScaleParts parts.
+// The largest scales of a cache's rows that some query sees, in kScaleParts parts.
 template <int D>
 __global__ void __launch_bounds__(256) packed_scales_kernel(BlockArgs16 a) {
   using L = PackedLayout<D>;
@@ -76,7 +76,22 @@ __global__ void __launch_bounds__(256) packed_scales_kernel(BlockArgs16 a) {
 #pragma unroll 4
   for (int t = t0 + part * kTilesPerStep + threadIdx.x / kPieces; t < t1; t += kScaleParts * kTilesPerStep) {
     const uint4 v = ld_global_16(base + (size_t)t * L::kBytes + L::kKeyScales + piece * 16);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const int lo_row = seen.lo - t * kPackedTile, hi_row = seen.len - t * kPackedTile;   // rows [lo_row, hi_row) of the tile are seen
+    if (lo_row > 0 || hi_row < kPackedTile) {
+      // the others may hold anything: the scales (at most two rows to a word) of those are taken as 0
+      auto kept = [&](int row) { return row >= lo_row && row < hi_row; };
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int word = (piece % (kPieces / 2)) * 4 + i;   // (of the key scales or of the value scales)
+        if (piece < kPieces / 2) {
+          if (!kept(word / (L::G / 2))) w[i] = 0;
+        } else {
+          const int row = word / (8 * L::G) * 16 + word / L::G % 2 * 8 + word / (2 * L::G) % 4;   // (value_scale the other way round)
+          w[i] &= (kept(row) ? 0x0000ffffu : 0u) | (kept(row + 4) ? 0xffff0000u : 0u);
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;

@@ -46,3 +46,30 @@ def test_lengths_far_below_zero_read_as_zeros(dtype):
             want[:3] = 0
             want[4, max(0, 50 - row0):] = 0
             same(got, want)
+
+
+def hidden_rows(b, Hq, Hkv, d, I, dtype, path):
+    """Rows behind the length or before the first row change nothing, however large: not the outputs' digits, not one bit."""
+    gen = torch.Generator("cuda").manual_seed(2)
+    n, lens, first = 200, [137, 200, 130, 165], [5, 67, 0, 31]
+    lens, first = [lens[s % 4] for s in range(b)], [first[s % 4] for s in range(b)]
+    row = torch.arange(n, device="cuda")
+    visible = ((row < ints(lens)[:, None]) & (row >= ints(first)[:, None]))[..., None, None]
+    k, v = normal(gen, b, n, Hkv, d) * 1e-4, normal(gen, b, n, Hkv, d) * 1e-4
+    q = (normal(gen, b, I, Hq, d) * 1e4).to(DT[dtype])
+    outs = []
+    for hidden in (0.0, 1.0, 5e5, 3e38):
+        kh, vh = (torch.where(visible, x, hidden * torch.sign(x)).to(DT[dtype]) for x in (k, v))
+        cache = make(b, Hq, Hkv, d, n, dtype, queries_max=I)
+        cache.write(kh, vh)
+        outs.append(cache.attend(q, ints(lens), first=ints(first)))
+        assert bm.last_packed_path() == path
+    want = exact(q, k.to(DT[dtype]), v.to(DT[dtype]), lens, first, d ** -0.5)
+    allowed = DIGITS if dtype == "bf16" else 2.0 ** -18
+    assert max((o.double() - want).norm() / want.norm() for o in outs) <= allowed
+    assert all(torch.equal(o, outs[0]) for o in outs)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_are_not_seen_change_nothing_in_blocks(d):
+    hidden_rows(40, 2, 2, d, 128, "bf16", 1)
