@@ -462,13 +462,14 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
 #pragma unroll
         for (int i = 0; i < G / 2; ++i) over |= (sc[i] & 0x7fff7fffu) + over_add;
         if (__any_sync(0xffffffffu, (over & 0x80008000u) != 0)) {
-          uint32_t largest = 0;
+          uint32_t largest = 0;   // of rows that some query of this tile sees: the others may hold anything, and get weights of 0
+          const bool counts = !kMasked || (row0 + lane >= lo && row0 + lane < most_rows);
 #pragma unroll
           for (int gi = 0; gi < G; ++gi) {   // lane = row
             unsigned short* place = reinterpret_cast<unsigned short*>(in + L::value_scale(lane, gi));
             const uint32_t mag = *place & 0x7fffu;
             const uint32_t bad = __ballot_sync(0xffffffffu, mag >= 0x7c00u);
-            largest = max(largest, mag >= 0x7c00u ? 0u : mag);
+            largest = max(largest, !counts || mag >= 0x7c00u ? 0u : mag);
             // A group whose scale is not finite is NaN for the queries that see it and nothing for the others: its scale becomes 0 in
             // the slot, and the group's outputs of those queries NaN.
             if (bad != 0) {

@@ -73,3 +73,9 @@ def hidden_rows(b, Hq, Hkv, d, I, dtype, path):
 @pytest.mark.parametrize("d", [64, 128])
 def test_rows_that_are_not_seen_change_nothing_in_blocks(d):
     hidden_rows(40, 2, 2, d, 128, "bf16", 1)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,I,dtype", [(4, 1, 1, "bf16"), (2, 2, 2, "bf16"), (8, 1, 1, "bf16"), (4, 2, 7, "bf16"), (4, 2, 1, "f32"), (2, 2, 9, "f32")])
+def test_rows_that_are_not_seen_change_nothing(Hq, Hkv, I, dtype, d):
+    hidden_rows(4, Hq, Hkv, d, I, dtype, 0)
