@@ -11,17 +11,18 @@
 // (subnormals, which the multiplication takes as they are), AND 0x00f000f0 two as u * 2^-20; a shift by 8 gives the other four.  AND
 // 0x0f0f0f0f it holds four bytes, shifted by 4 the other four: half the work, where the other side of the product can be 8-bit integers.
 // It can for up to four query rows, as two numbers each in two of the eight columns: q = 256 hi + lo, 15 bits with the sign for the row's
-// largest element.  No addition takes the 8 away: sum u q = sum code q + 8 sum q, so integer sums start at -8 sum q, fp32 ones at the sum over
-// the groups of s * (-8 sum q), one small MMA of the scales and the queries' sums; P.V counts the sum of its own rounded weights with one
-// more MMA per group.  What that costs is digits: sums of up to 23 times what remains, at fp32's step.  It is far below the rounding of bf16
-// outputs, and 30 times above that of fp32 ones (relative error 5e-6 measured), so fp32 caches take the codes themselves as fp16 numbers,
-// one fp16 addition per pair, and join P.V's sums tile by tile outside the MMA.
+// largest element; a row whose largest element stands out gets 8 more in products of their own (kUneven).  No addition takes the 8 away:
+// sum u q = sum code q + 8 sum q, so integer sums start at -8 sum q, fp32 ones at the sum over the groups of s * (-8 sum q), one small MMA
+// of the scales and the queries' sums; P.V counts the sum of its own rounded weights with one more MMA per group.  What that costs is
+// digits: sums of up to 23 times what remains, at fp32's step.  It is far below the rounding of bf16 outputs, and 30 times above that of
+// fp32 ones (relative error 5e-6 measured), so fp32 caches take the codes themselves as fp16 numbers, one fp16 addition per pair, and join
+// P.V's sums tile by tile outside the MMA.
 //
-// Numbers: a query row is brought to a largest magnitude of 2^13 .. 2^14 by a power of two for the integers (an element is off by 1/2, 2^-15
-// of the largest), of 2^14 .. 2^15 for fp16, where bf16 values are exact (fp32: two numbers, 22 bits).  Weights are p * 2^shift (fp16, 11
-// bits; two numbers for fp32) times the value's scale (fp32: and 2^lift, for scales far below 1); shift is 12, less where a scale of 2 or
-// more would pass fp16.  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.  Softmax statistics and all
-// sums are fp32.
+// Numbers: a query row is brought to a largest magnitude of 2^13 .. 2^14 by a power of two for the integers (an element is off by 1/2 at
+// most, by 1/256 with the third number), of 2^14 .. 2^15 for fp16, where bf16 values are exact (fp32: two numbers, 22 bits).  Weights are
+// p * 2^shift (fp16, 11 bits; two numbers for fp32) times the value's scale (fp32: and 2^lift, for scales far below 1); shift is 12, less
+// where a scale of 2 or more would pass fp16.  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.  Softmax
+// statistics and all sums are fp32.
 //
 // Work: the tiles of all caches of the call, one after another, are cut into equal runs, so that samples of unequal length cost no idle
 // SMs and few long caches are shared by all.  A run is one warp's, which streams it through a ring of shared memory (one
@@ -48,6 +49,11 @@ constexpr int kWarps = 2;                     // independent of each other; one 
 constexpr int kWarpsPerSm = 12;
 constexpr int kMostSms = 148;                 // that the workspace is sized for
 constexpr int kFullShift = 12;
+// Queries as integers: a row whose largest element is more than this many times the mean of its magnitudes (3.6 for normal values) gets a
+// third number of 8 bits.  Without it an element is off by 2^-14 of the largest at most, so by 2^-11 of the mean: what fp16 does to weights.
+// For such rows a tile costs 8 more MMAs, on a way of their own.  (Three numbers for every row: 384 samples of 1535 rows, 32 / 8 heads,
+// d = 128, 127 us, two 117, two with this way beside them 119; d = 64 97, 94, 94.)
+constexpr float kUneven = 8.f;
 
 __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, const float* c) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
@@ -55,10 +61,10 @@ __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, ui
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 // a: bytes without sign, b: with
-__device__ __forceinline__ void mma_u8s8(int* d, const uint32_t* a, uint32_t b0, uint32_t b1, int even, int odd) {
-  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+__device__ __forceinline__ void mma_u8s8(int* d, const uint32_t* a, uint32_t b0, uint32_t b1, const uint32_t* c) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
       : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(even), "r"(odd));
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]));
 }
 // d = a (16 x 8) * b (8 x 8)
 __device__ __forceinline__ void mma_k8(float* d, uint32_t a0, uint32_t a1, uint32_t b) {
@@ -154,7 +160,11 @@ struct Attend {
   // 122, 10 137; four slots 121 against 118.
   static constexpr int kStages = 3, kResident = kWarpsPerSm;
   static constexpr int kQueryWords = kSigned ? 8 * G : PAIR ? 2 * G : 4 * G;   // B fragments of Q, words of a lane
-  static constexpr int kWarpBytes = kStages * PackedLayout<D>::kBytes, kSmem = kWarps * kWarpBytes;
+  static constexpr int kWarpBytes = kStages * PackedLayout<D>::kBytes;
+  // Shared memory of PAIR beside the ring: words that a lane has for its queries' third numbers, [group][b0, b1] and -8 times their sums
+  // [group]; per warp what the other integer sums start at, quads of an MMA's C [group][c] (which would take 16 registers).
+  static constexpr int kThirdWords = PAIR ? (3 * G + 3) / 4 * 4 : 0, kThirdBytes = kThirdWords * 4 * 32, kStartBytes = PAIR ? G * 4 * 16 : 0;
+  static constexpr int kSmem = kWarps * (kWarpBytes + kThirdBytes + kStartBytes);
   static_assert(!PAIR || !kSigned, "");
 };
 
@@ -237,6 +247,12 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, r = lane / 4, c = lane % 4, run = blockIdx.x * kWarps + warp;
   unsigned char* ring = smem + warp * A::kWarpBytes;
   uint64_t* bar = bars[warp];
+  [[maybe_unused]] auto start_at = [&](int gi) {   // this lane's quad
+    return reinterpret_cast<int4*>(smem + kWarps * (A::kWarpBytes + A::kThirdBytes)) + (warp * G + gi) * 4 + c;
+  };
+  [[maybe_unused]] auto third_at = [&](int i) {    // this lane's word i
+    return reinterpret_cast<int*>(smem + kWarps * A::kWarpBytes) + ((i / 4) * kWarps * 32 + (int)threadIdx.x) * 4 + i % 4;
+  };
   if (lane == 0) {
     for (int i = 0; i < kStages; ++i) tc::mbar_init(&bar[i], 1);
     tc::mbar_fence_init();
@@ -330,14 +346,15 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
     const int least = len - (a.I - 1 - a.by_g(col0)), most_rows = len - (a.I - 1 - a.by_g(col0 + cols_here - 1));
     uint32_t bq[A::kQueryWords];                 // [number][group][two k-steps][b0, b1], integers: [group][b0, b1]
     uint32_t start = 0;                          // B fragment of the -8 sum q: two fp16 numbers for each group
-    int start_int[PAIR ? G : 1][2];              // -8 sum of hi, of lo, of this lane's column
     float colmul[C];                             // of this lane's columns
     [[maybe_unused]] float not_finite = 0.f;     // integers: NaN where the column's query is not finite
+    [[maybe_unused]] bool third = false;         // integers: some query of the tile has a third number
     {
       const int col = col0 + (PAIR ? r / 2 : r), query = a.by_g(col);
       const T* q = static_cast<const T*>(a.q) + at.smp * a.q_sample + query * a.q_token + ((size_t)at.head * a.c.g + col - query * a.c.g) * D + 8 * c;
       float x[G][8];
       uint32_t most_bits = 0;   // magnitudes compare as integers, what is not finite above the rest
+      [[maybe_unused]] float mean = 0.f;   // of the magnitudes
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
 #pragma unroll
@@ -348,9 +365,19 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) most_bits = max(most_bits, __float_as_uint(x[gi][j]) & 0x7fffffffu);
+        if constexpr (PAIR) {   // (divided first, so that no sum is infinite)
+          float part = 0.f;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) part = fmaf(fabsf(x[gi][j]), 1.f / D, part);
+          mean += part;
+        }
       }
       most_bits = max(most_bits, __shfl_xor_sync(0xffffffffu, most_bits, 1));
       most_bits = max(most_bits, __shfl_xor_sync(0xffffffffu, most_bits, 2));
+      if constexpr (PAIR) {
+        mean += __shfl_xor_sync(0xffffffffu, mean, 1);
+        mean += __shfl_xor_sync(0xffffffffu, mean, 2);
+      }
       // the largest magnitude to its place; a row that is not finite has NaN logits
       const bool finite = most_bits < 0x7f800000u;
       const int e = finite && most_bits > 0 ? min((PAIR ? 13 : 14) - (int)(most_bits >> 23) + 127, 100) : 0;
@@ -376,8 +403,31 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
           }
           sum += __shfl_xor_sync(0xffffffffu, sum, 1);
           sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-          start_int[gi][0] = -8 * __shfl_sync(0xffffffffu, sum, 8 * c);
-          start_int[gi][1] = -8 * __shfl_sync(0xffffffffu, sum, 8 * c + 4) + kMagic;
+          const int of_hi = -8 * __shfl_sync(0xffffffffu, sum, 8 * c), of_lo = -8 * __shfl_sync(0xffffffffu, sum, 8 * c + 4) + kMagic;
+          if (r == 0) *start_at(gi) = make_int4(of_hi, of_lo, of_hi, of_lo);
+        }
+        third = __any_sync(0xffffffffu, finite && __uint_as_float(most_bits) * (1.f / kUneven) > mean);
+        if (third) {
+          // what rounding to integers left, in 256ths (a half would be 128 of them: 127)
+#pragma unroll
+          for (int gi = 0; gi < G; ++gi) {
+            int sum = 0;
+#pragma unroll
+            for (int odd = 0; odd < 2; ++odd) {
+              uint32_t y[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float v = x[gi][2 * j + odd] * up, left = v - ((v + __int_as_float(kMagic)) - __int_as_float(kMagic));
+                y[j] = __float_as_uint(fminf(left * 256.f, 127.f) + __int_as_float(kMagic));   // (its low byte)
+              }
+              const uint32_t b = __byte_perm(__byte_perm(y[0], y[1], 0x0040), __byte_perm(y[2], y[3], 0x0040), 0x5410);
+              *third_at(2 * gi + odd) = r % 2 ? 0 : (int)b;
+              sum = __dp4a((int)b, 0x01010101, sum);
+            }
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            *third_at(2 * G + gi) = -8 * __shfl_sync(0xffffffffu, sum, 8 * c);
+          }
         }
       } else {
         float sums[G];
@@ -415,6 +465,7 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
       }
 #pragma unroll
       for (int j = 0; j < C; ++j) colmul[j] = __shfl_sync(0xffffffffu, mul, 4 * (2 * c + j));   // from this lane's column to the sums'
+      __syncwarp();
     }
     auto column = [&](int j) { return PAIR ? c : 2 * c + j; };   // of the sums, from col0
 
@@ -532,7 +583,9 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
           if constexpr (PAIR) {
             const uint32_t a0[4] = {w0[gi] & 0x0f0f0f0fu, w1[gi] & 0x0f0f0f0fu, w0[gi] >> 4 & 0x0f0f0f0fu, w1[gi] >> 4 & 0x0f0f0f0fu};
             int acc[4];
-            mma_u8s8(acc, a0, bq[2 * gi], bq[2 * gi + 1], start_int[gi][0], start_int[gi][1]);
+            uint32_t from8[4];
+            lds<4>(start_at(gi), from8);
+            mma_u8s8(acc, a0, bq[2 * gi], bq[2 * gi + 1], from8);
             // |sum code q| < 32 * 8 * 2^14 = 2^22
             s[sub][0][0] = fmaf(s0, __int_as_float(acc[0] * 256 + acc[1]) - __int_as_float(kMagic), s[sub][0][0]);
             s[sub][1][0] = fmaf(s1, __int_as_float(acc[2] * 256 + acc[3]) - __int_as_float(kMagic), s[sub][1][0]);
@@ -558,7 +611,7 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
       }
 
       // ---- softmax, running -----------------------------------------------------------------------------------------------------
-      bool grown = false;
+      bool grown = PAIR && third;
       float top[C];
 #pragma unroll
       for (int j = 0; j < C; ++j) {
@@ -576,6 +629,30 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
         grown |= top[j] > m[j] + 2.f;
       }
       if (__any_sync(0xffffffffu, grown)) {
+        if constexpr (PAIR) {
+          if (third) {   // (rare: what this needs is fetched again, so that nothing is kept for it)
+#pragma unroll 1
+            for (int i = 0; i < 2 * G; ++i) {
+              const int sub = i / G, gi = i % G, key = sub * 16 + r / 2 + 4 * (r % 2);
+              uint32_t w0, w1;
+              lds<1>(in + key * (D / 2) + (c * G + gi) * 4, &w0);
+              lds<1>(in + (key + 8) * (D / 2) + (c * G + gi) * 4, &w1);
+              const uint32_t a0[4] = {w0 & 0x0f0f0f0fu, w1 & 0x0f0f0f0fu, w0 >> 4 & 0x0f0f0f0fu, w1 >> 4 & 0x0f0f0f0fu};
+              int acc[4];
+              const uint32_t from = (uint32_t)*third_at(2 * G + gi), start3[4] = {from, 0u, from, 0u};
+              mma_u8s8(acc, a0, (uint32_t)*third_at(gi * 2), (uint32_t)*third_at(gi * 2 + 1), start3);
+              const __half* sc = reinterpret_cast<const __half*>(in + L::kKeyScales) + key * G + gi;
+              // (hidden logits stay -inf, whatever the row's scale)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float d = __half2float(sc[8 * G * k]) * (0x1p-8f * (float)acc[2 * k]);
+                if (sub == 0 && s[0][k][0] != -INFINITY) s[0][k][0] += d;
+                if (sub == 1 && s[1][k][0] != -INFINITY) s[1][k][0] += d;
+              }
+            }
+            top[0] = fmaxf(fmaxf(s[0][0][0], s[0][1][0]), fmaxf(s[1][0][0], s[1][1][0])) * colmul[0];
+          }
+        }
         float k[C];
 #pragma unroll
         for (int j = 0; j < C; ++j) {

@@ -79,3 +79,28 @@ def test_rows_that_are_not_seen_change_nothing_in_blocks(d):
 @pytest.mark.parametrize("Hq,Hkv,I,dtype", [(4, 1, 1, "bf16"), (2, 2, 2, "bf16"), (8, 1, 1, "bf16"), (4, 2, 7, "bf16"), (4, 2, 1, "f32"), (2, 2, 9, "f32")])
 def test_rows_that_are_not_seen_change_nothing(Hq, Hkv, I, dtype, d):
     hidden_rows(4, Hq, Hkv, d, I, dtype, 0)
+
+
+SHAPES = [(2, 1, 1, 1, 1000, 0), (2, 4, 1, 1, 1000, 0), (2, 2, 1, 2, 1000, 0), (2, 8, 1, 1, 1000, 0), (2, 4, 1, 6, 1000, 0), (40, 2, 2, 128, 400, 1)]
+
+
+@pytest.mark.parametrize("r", [30.0, 100.0, 1000.0])
+@pytest.mark.parametrize("b,Hq,Hkv,I,n,path", SHAPES)
+def test_queries_with_an_outlier(b, Hq, Hkv, I, n, path, r):
+    """One channel of the queries r times the others, and that channel of the keys an r-th: logits are as without, so their digits are
+    those that the other channels keep beside the outlier.  Steps of 2^-21 of the outlier leave 1000 * 2^-21 / sqrt(12) of them, and of the
+    logits, which have a deviation of 3, 5e-4."""
+    gen = torch.Generator("cuda").manual_seed(3)
+    q, k, v = normal(gen, b, I, Hq, 128), normal(gen, b, n, Hkv, 128), normal(gen, b, n, Hkv, 128)
+    q[..., 5] *= r
+    k[..., 5] /= r
+    k[..., 40:] *= 4.0
+    k[1::2, n - 77:] = v[1::2, n - 77:] = torch.nan      # (behind their samples' lengths)
+    q, k, v = q.bfloat16(), k.bfloat16(), v.bfloat16()
+    cache = make(b, Hq, Hkv, 128, n, "bf16", queries_max=I)
+    cache.write(k, v)
+    lens = [n, n - 77] * (b // 2)
+    out = cache.attend(q, ints(lens))
+    assert bm.last_packed_path() == path
+    want = exact(q, k, v, lens, [0] * b, 128 ** -0.5)
+    assert (out.double() - want).norm() <= DIGITS * want.norm()
