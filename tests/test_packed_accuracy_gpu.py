@@ -104,3 +104,27 @@ def test_queries_with_an_outlier(b, Hq, Hkv, I, n, path, r):
     assert bm.last_packed_path() == path
     want = exact(q, k, v, lens, [0] * b, 128 ** -0.5)
     assert (out.double() - want).norm() <= DIGITS * want.norm()
+
+
+@pytest.mark.parametrize("scale", [0.0, 0.35, 1.0])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("b,Hq,Hkv,I,n,path", [(4, 4, 4, 1, 1500, 0), (4, 8, 2, 1, 1500, 0), (4, 16, 2, 1, 1500, 0), (4, 8, 2, 2, 700, 0),
+                                               (4, 10, 2, 3, 700, 0), (40, 2, 2, 128, 400, 1), (20, 8, 4, 150, 400, None)])
+def test_outputs_are_the_rounded_exact_ones_but_for_few_digits(b, Hq, Hkv, I, n, path, d, scale):
+    """Without the rounding of the outputs, errors are those of the weights: each is rounded to fp16 (a half step is 2^-12 to 2^-11 of it,
+    2.0e-4 in the mean square), and outside of blocks once more with its row's scale: 2.9e-4 of an output where few rows make it up, less
+    where many do.  Twice that is allowed, over at least 16 outputs' mean square.  (Logits' errors, 2^-18 of them at most, do not show.  A
+    tile of values with 8 bits would leave 1.6e-3.)"""
+    gen = torch.Generator("cuda").manual_seed(4)
+    q, k, v = (normal(gen, b, t, h, d).bfloat16() for t, h in ((I, Hq), (n, Hkv), (n, Hkv)))
+    cache = make(b, Hq, Hkv, d, n, "bf16", queries_max=I, softmax_scale=scale)
+    cache.write(k, v)
+    lens = [n, n - 77] * (b // 2)
+    out, took = cache.attend(q, ints(lens)).double(), bm.last_packed_path()
+    assert path in (took, None)
+    want = exact(q, k, v, lens, [0] * b, scale or d ** -0.5)
+    rounded = want.bfloat16().double()
+    # errors of the outputs' rounding and of what is rounded are independent: their squares add up
+    inner = (out - want).square().sum() - (rounded - want).square().sum()
+    assert inner <= (4e-4 if took == 1 else 6e-4) ** 2 * want.square().sum()
+    assert (out - want).norm() <= DIGITS * want.norm()
