@@ -469,7 +469,9 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
     }
     auto column = [&](int j) { return PAIR ? c : 2 * c + j; };   // of the sums, from col0
 
-    float m[C], mneg[C], l[C], o[G][2][4], ow[4];   // mneg = shift - m
+    // Weights are 2^(logit + mneg), mneg = shift - m rounded down: where m leaves no room for the shift they are the smaller ones, and all that
+    // was summed with another mneg follows by the difference of the two.
+    float m[C], mneg[C], l[C], o[G][2][4], ow[4];
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       m[j] = -INFINITY;
@@ -540,14 +542,17 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
           const int next = min(shift + lift, 12 - ((int)(largest >> 10) - 15));   // the largest scale is below 2^(13 - shift - lift)
           if (next < shift + lift) {
             const int next_shift = min(next, kFullShift);
-            const float k = pow2(next_shift - shift), k_lift = pow2(next - next_shift - lift);
-            const float ks[2] = {k, k};
+            const float k_lift = pow2(next - next_shift - lift);
+            float ks[C];
             [[maybe_unused]] const float ks_lift[2] = {k_lift, k_lift};
+#pragma unroll
+            for (int j = 0; j < C; ++j) {
+              const float before = mneg[j];
+              if (m[j] != -INFINITY) mneg[j] = __fsub_rd((float)next_shift, m[j]);
+              ks[j] = exp2_approx(mneg[j] - before);
+            }
             rescale(ks);
             if constexpr (kSigned) rescale_outputs(ks_lift);
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-              if (m[j] != -INFINITY) mneg[j] = (float)next_shift - m[j];
             shift = next_shift;
             lift = next - next_shift;
             over_add = over_of(next);
@@ -660,9 +665,10 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
           t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 4));
           t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 8));
           t = fmaxf(m[j], fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 16)));
-          k[j] = m[j] == t ? 1.f : exp2_approx(m[j] - t);   // (both -inf: nothing seen yet)
+          const float next = t == -INFINITY ? 0.f : __fsub_rd((float)shift, t);
+          k[j] = m[j] == -INFINITY ? 1.f : exp2_approx(next - mneg[j]);   // (nothing seen yet: nothing summed)
           m[j] = t;
-          mneg[j] = t == -INFINITY ? 0.f : (float)shift - t;
+          mneg[j] = next;
         }
         rescale(k);
       }
@@ -675,7 +681,10 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
           float p[2] = {0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < C; ++j) {
-            p[j] = exp2_approx(fmaf(s[sub][k][j], colmul[j], mneg[j]));
+            // The logit is rounded before m is taken off, as m was: a largest one of 2^25 may be 2 above its rounded self, one of 2^30 64.  fp32
+            // has its last digits of smaller ones without.
+            const float rounded = __fadd_rn(__fmul_rn(s[sub][k][j], colmul[j]), mneg[j]);
+            p[j] = exp2_approx(kSigned && fabsf(mneg[j]) < 0x1p18f ? fmaf(s[sub][k][j], colmul[j], mneg[j]) : rounded);
             l[j] += p[j];
           }
           const uint32_t h = pack(p[0], p[1]);
@@ -780,8 +789,9 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
           else store4(to + cc * (D + 4) + 32 * gi + 4 * r, x0, x1, x2, x3);
         }
       }
-      // the weights are 2^shift times p to the maximum m
-      if (!whole && r == 0 && cc < cols_here) *reinterpret_cast<float2*>(to + cc * (D + 4) + D) = make_float2(m[j] - (float)shift, l[j]);
+      // what the weights are relative to
+      if (!whole && r == 0 && cc < cols_here)
+        *reinterpret_cast<float2*>(to + cc * (D + 4) + D) = make_float2(m[j] == -INFINITY ? m[j] : -mneg[j], l[j]);
     }
     left -= share;
     if (left > 0) at.next_cache(a);

@@ -128,3 +128,36 @@ def test_outputs_are_the_rounded_exact_ones_but_for_few_digits(b, Hq, Hkv, I, n,
     inner = (out - want).square().sum() - (rounded - want).square().sum()
     assert inner <= (4e-4 if took == 1 else 6e-4) ** 2 * want.square().sum()
     assert (out - want).norm() <= DIGITS * want.norm()
+
+
+@pytest.mark.parametrize("Hq,I,dtype", [(4, 1, "bf16"), (8, 1, "bf16"), (2, 9, "bf16"), (4, 1, "f32")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("size", [2.0 ** 26])
+def test_logits_next_to_the_largest_number(size, Hq, I, dtype, d):
+    """Queries of 2^121: their logits are numbers of 32 bits, and the row with the largest takes the whole weight."""
+    gen = torch.Generator("cuda").manual_seed(6)
+    n = 60
+    q, k, v = (normal(gen, 1, I, Hq, d) * size).to(DT[dtype]), normal(gen, 1, n, 1, d).to(DT[dtype]), normal(gen, 1, n, 1, d).to(DT[dtype])
+    q[0, 0, 0] = 0.0                       # (a mean over all rows)
+    cache = make(1, Hq, 1, d, n, dtype, queries_max=I)
+    cache.write(k, v)
+    out = cache.attend(q, ints([n]))
+    want = exact(q, k, v, [n], [0], d ** -0.5)
+    assert out.isfinite().all()
+    assert (out.double() - want).norm() <= (DIGITS if dtype == "bf16" else 2.0 ** -18) * want.norm()
+
+
+@pytest.mark.parametrize("Hq,I,dtype", [(4, 1, "bf16"), (8, 1, "bf16"), (4, 1, "f32"), (2, 9, "f32")])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 18, 2.0 ** 23, 2.0 ** 26, 2.0 ** 100])
+def test_equal_logits_of_any_size(size, Hq, I, dtype):
+    """Rows with one key share the weight evenly, also where their values' scales change on the way and the logit leaves no room for them."""
+    gen = torch.Generator("cuda").manual_seed(10)
+    n, d = 700, 128
+    q, k = (normal(gen, 1, I, Hq, d) * size).to(DT[dtype]), normal(gen, 1, 1, 1, d).expand(1, n, 1, d).to(DT[dtype])
+    v = (normal(gen, 1, n, 1, d) + 1.0) * 2.0 ** (torch.arange(n, device="cuda") // 50)[:, None, None]
+    v = v.to(DT[dtype])
+    cache = make(1, Hq, 1, d, n, dtype, queries_max=I)
+    cache.write(k.contiguous(), v)
+    out = cache.attend(q, ints([n]))
+    want = exact(torch.zeros_like(q), k, v, [n], [0], 1.0)
+    assert (out.double() - want).norm() <= (DIGITS if dtype == "bf16" else 2.0 ** -18) * want.norm()
