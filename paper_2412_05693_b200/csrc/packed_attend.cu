@@ -383,7 +383,9 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
       const int e = finite && most_bits > 0 ? min((PAIR ? 13 : 14) - (int)(most_bits >> 23) + 127, 100) : 0;
       if constexpr (PAIR) not_finite = __shfl_sync(0xffffffffu, finite ? 0.f : __int_as_float(0x7fffffff), 8 * c);
       const float up = pow2(e);
-      const float mul = fmaxf(a.mul * kKey * pow2(-e), 0x1p-126f);   // (above 0: times -inf it stays -inf)
+      // Above 0: times -inf it stays -inf.  Finite: next to the largest queries it may be above fp32, where the codes' 2^-24 makes up for it; logits
+      // are 2^50 apart then or equal, with the largest number in its place too.
+      const float mul = fminf(fmaxf(a.mul * kKey * pow2(-e), 0x1p-126f), 0x1.fffffep127f);
       if constexpr (PAIR) {
 #pragma unroll
         for (int gi = 0; gi < G; ++gi) {

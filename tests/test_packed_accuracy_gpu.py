@@ -132,7 +132,7 @@ def test_outputs_are_the_rounded_exact_ones_but_for_few_digits(b, Hq, Hkv, I, n,
 
 @pytest.mark.parametrize("Hq,I,dtype", [(4, 1, "bf16"), (8, 1, "bf16"), (2, 9, "bf16"), (4, 1, "f32")])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("size", [2.0 ** 26])
+@pytest.mark.parametrize("size", [2.0 ** 26, 2.0 ** 121])
 def test_logits_next_to_the_largest_number(size, Hq, I, dtype, d):
     """Queries of 2^121: their logits are numbers of 32 bits, and the row with the largest takes the whole weight."""
     gen = torch.Generator("cuda").manual_seed(6)
