@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
       }
       const int e = most > 0 && most < 0x7f800000u ? min(14 - (int)(most >> 23) + 127, 100) : 0;
       const float up = pow2(e);
-      row_mul = fmaxf(a.mul * pow2(-e) * pow2(-ek), 0x1p-126f);
+      row_mul = fminf(fmaxf(a.mul * pow2(-e) * pow2(-ek), 0x1p-126f), 0x1.fffffep127f);
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) {
         float f[8];
@@ -464,6 +464,16 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
         l *= alpha;
       }
       const float neg_m = m_used == -INFINITY ? 0.f : -m_used;   // (no row seen so far)
+      // Below, m_used is taken from the exact product of a logit and row_mul, which is up to 2^-24 of it away from the rounded one that m_used is:
+      // where that is not next to nothing, logits are rounded first, as m_used was.
+      float mul = row_mul;
+      if (__any_sync(0xffffffffu, fabsf(neg_m) > 0x1p20f)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[c][e] = __float_as_uint(__fmul_rn(__uint_as_float(s[c][e]), row_mul));
+        mul = 1.f;
+      }
       float pa0 = 0.f, pa1 = 0.f, pb0 = 0.f, pb1 = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
@@ -471,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) packed_block_kernel(BlockArgs16 a
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           float x0, x1;
-          fma2(x0, x1, __uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1]), row_mul, neg_m);
+          fma2(x0, x1, __uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1]), mul, neg_m);
           const float p0 = ex2(x0), p1 = ex2(x1);
           if (e & 1) add2(pb0, pb1, p0, p1);
           else add2(pa0, pa1, p0, p1);

@@ -161,3 +161,20 @@ def test_equal_logits_of_any_size(size, Hq, I, dtype):
     out = cache.attend(q, ints([n]))
     want = exact(torch.zeros_like(q), k, v, [n], [0], 1.0)
     assert (out.double() - want).norm() <= (DIGITS if dtype == "bf16" else 2.0 ** -18) * want.norm()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 26, 2.0 ** 121])
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_next_to_the_largest_number_in_blocks(d, size):
+    gen = torch.Generator("cuda").manual_seed(9)
+    b, I, n = 40, 128, 300
+    q, k, v = (normal(gen, b, I, 2, d) * size).bfloat16(), normal(gen, b, n, 2, d).bfloat16(), normal(gen, b, n, 2, d).bfloat16()
+    q[:, 3] = 0.0
+    cache = make(b, 2, 2, d, n, "bf16", queries_max=I)
+    cache.write(k, v)
+    lens = [300, 270] * 20
+    out = cache.attend(q, ints(lens))
+    assert bm.last_packed_path() == 1
+    want = exact(q, k, v, lens, [0] * b, d ** -0.5)
+    assert out.isfinite().all()
+    assert (out.double() - want).norm() <= DIGITS * want.norm()
