@@ -20,8 +20,8 @@
 //
 // Numbers: a query row is brought to a largest magnitude of 2^13 .. 2^14 by a power of two for the integers (an element is off by 1/2 at
 // most, by 1/256 with the third number), of 2^14 .. 2^15 for fp16, where bf16 values are exact (fp32: two numbers, 22 bits).  Weights are
-// p * 2^shift (fp16, 11 bits; two numbers for fp32) times the value's scale (fp32: and 2^lift, for scales far below 1); shift is 12, less
-// where a scale of 2 or more would pass fp16.  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.  Softmax
+// p * 2^shift (fp16, 11 bits; two numbers for fp32) times the value's scale; shift is 12, less where a scale of 2 or more would pass fp16
+// (fp32: it stays, and a group's scales are taken times 2^lift, so that the largest of a group so far is where it keeps both numbers).  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.  Softmax
 // statistics and all sums are fp32.
 //
 // Work: the tiles of all caches of the call, one after another, are cut into equal runs, so that samples of unequal length cost no idle
@@ -486,25 +486,28 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
 #pragma unroll
       for (int k = 0; k < 8; ++k) o[gi][k / 4][k % 4] = 0.f;
     int shift = kFullShift;
-    [[maybe_unused]] int lift = kSigned ? 15 : 0;   // fp32: the value scales are taken times 2^lift, so that small ones keep their second number
+    // fp32: the shift stays, and every group's value scales are taken times a power of two of its own, so that small ones keep their second number
+    [[maybe_unused]] int lift[G];
+#pragma unroll
+    for (int gi = 0; gi < G; ++gi) lift[gi] = kSigned ? 15 : 0;
     auto over_of = [](int total) { return 0x7fff7fffu - 0x00010001u * (((28 - total) << 10) - 1); };
-    uint32_t over_add = over_of(shift + lift);      // carries into bit 15 what is 2^(13 - shift - lift) or more
+    constexpr int kOvers = kSigned ? G / 2 : 1;
+    uint32_t over_add[kOvers];                      // carries into bit 15 what is 2^(13 - shift - lift) or more (fp32: of the lane's words)
+#pragma unroll
+    for (int i = 0; i < kOvers; ++i) over_add[i] = over_of(shift + (kSigned ? 15 : 0));
 
-    auto rescale_outputs = [&](const float* k) {
-#pragma unroll
-      for (int gi = 0; gi < G; ++gi)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < C; ++j) o[gi][i / 2][2 * (i % 2) + j] *= k[j];
-    };
     auto rescale = [&](const float* k) {   // everything that was summed with the weights
 #pragma unroll
       for (int j = 0; j < C; ++j) {
         l[j] *= k[j];
         if constexpr (!kSigned) ow[j] *= k[j];
       }
-      rescale_outputs(k);
+#pragma unroll
+      for (int gi = 0; gi < G; ++gi)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < C; ++j) o[gi][i / 2][2 * (i % 2) + j] *= k[j];
     };
 
     auto tile = [&](auto masked_tag, int row0, unsigned char* in) {
@@ -515,7 +518,7 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
         uint32_t sc[G / 2], over = 0;
         lds<G / 2>(in + L::kValueScales + lane * 2 * G, sc);
 #pragma unroll
-        for (int i = 0; i < G / 2; ++i) over |= (sc[i] & 0x7fff7fffu) + over_add;
+        for (int i = 0; i < G / 2; ++i) over |= (sc[i] & 0x7fff7fffu) + over_add[i % kOvers];
         if (__any_sync(0xffffffffu, (over & 0x80008000u) != 0)) {
           uint32_t largest = 0;   // of rows that some query of this tile sees: the others may hold anything, and get weights of 0
           const bool counts = !kMasked || (row0 + lane >= lo && row0 + lane < most_rows);
@@ -524,7 +527,17 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
             unsigned short* place = reinterpret_cast<unsigned short*>(in + L::value_scale(lane, gi));
             const uint32_t mag = *place & 0x7fffu;
             const uint32_t bad = __ballot_sync(0xffffffffu, mag >= 0x7c00u);
-            largest = max(largest, !counts || mag >= 0x7c00u ? 0u : mag);
+            const uint32_t mine = !counts || mag >= 0x7c00u ? 0u : mag;
+            largest = max(largest, mine);
+            if constexpr (kSigned) {
+              const int next = min(shift + lift[gi], 12 - ((int)(__reduce_max_sync(0xffffffffu, mine) >> 10) - 15));
+              if (next < shift + lift[gi]) {
+                const float k = pow2(next - shift - lift[gi]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[gi][i / 4][i % 4] *= k;
+                lift[gi] = next - shift;
+              }
+            }
             // A group whose scale is not finite is NaN for the queries that see it and nothing for the others: its scale becomes 0 in
             // the slot, and the group's outputs of those queries NaN.
             if (bad != 0) {
@@ -540,24 +553,25 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
               }
             }
           }
-          largest = __reduce_max_sync(0xffffffffu, largest);
-          const int next = min(shift + lift, 12 - ((int)(largest >> 10) - 15));   // the largest scale is below 2^(13 - shift - lift)
-          if (next < shift + lift) {
-            const int next_shift = min(next, kFullShift);
-            const float k_lift = pow2(next - next_shift - lift);
-            float ks[C];
-            [[maybe_unused]] const float ks_lift[2] = {k_lift, k_lift};
+          if constexpr (kSigned) {
+            // the lane's words: of the groups lane % 2 * (G / 2) ..
 #pragma unroll
-            for (int j = 0; j < C; ++j) {
-              const float before = mneg[j];
-              if (m[j] != -INFINITY) mneg[j] = __fsub_rd((float)next_shift, m[j]);
-              ks[j] = exp2_approx(mneg[j] - before);
+            for (int i = 0; i < kOvers; ++i) over_add[i] = over_of(shift + (lane % 2 ? lift[G / 2 + i] : lift[i]));
+          } else {
+            largest = __reduce_max_sync(0xffffffffu, largest);
+            const int next = min(shift, 12 - ((int)(largest >> 10) - 15));   // the largest scale is below 2^(13 - shift)
+            if (next < shift) {
+              float ks[C];
+#pragma unroll
+              for (int j = 0; j < C; ++j) {
+                const float before = mneg[j];
+                if (m[j] != -INFINITY) mneg[j] = __fsub_rd((float)next, m[j]);
+                ks[j] = exp2_approx(mneg[j] - before);
+              }
+              rescale(ks);
+              shift = next;
+              over_add[0] = over_of(next);
             }
-            rescale(ks);
-            if constexpr (kSigned) rescale_outputs(ks_lift);
-            shift = next_shift;
-            lift = next - next_shift;
-            over_add = over_of(next);
           }
           tc::fence_async_smem();   // (the slot is filled by an asynchronous copy again)
           __syncwarp();
@@ -698,7 +712,6 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
         }
 
       // ---- outputs ---------------------------------------------------------------------------------------------------------------
-      [[maybe_unused]] const float lifted = pow2(lift);
       uint32_t v[2][2][G], sv[2][2][G];   // of the keys (c, c + 4) and (c + 8, c + 12) of every 16, a word per group
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
@@ -710,6 +723,7 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
         float part[2][4];
+        [[maybe_unused]] const float lifted = pow2(lift[gi]);
         if constexpr (kSigned) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) part[i / 4][i % 4] = 0.f;
@@ -779,11 +793,12 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
       if constexpr (PAIR)
         if (l[j] != 0.f) l[j] += not_finite;   // (seen something)
       const int cc = column(j), col = col0 + cc, query = a.by_g(col);
-      const float by = (whole ? (l[j] == 0.f ? 0.f : 1.f / l[j]) : 1.f) * pow2(-lift);   // (a query that sees no row has a row of zeros)
+      const float by_all = whole ? (l[j] == 0.f ? 0.f : 1.f / l[j]) : 1.f;   // (a query that sees no row has a row of zeros)
       T* out = static_cast<T*>(a.out) + (((size_t)at.smp * a.I + query) * a.c.Hq + (size_t)at.head * a.c.g + col - query * a.c.g) * D + 4 * r;
 #pragma unroll
       for (int gi = 0; gi < G; ++gi) {
         const float sum = kSigned ? 0.f : 8.f * __shfl_sync(0xffffffffu, ow[j], 4 * gi + c);
+        const float by = by_all * pow2(-lift[gi]);
         const float x0 = (o[gi][0][j] * kEven - sum) * by, x1 = (o[gi][0][2 + j] * kOdd - sum) * by;
         const float x2 = (o[gi][1][j] * kEven - sum) * by, x3 = (o[gi][1][2 + j] * kOdd - sum) * by;
         if (cc < cols_here) {

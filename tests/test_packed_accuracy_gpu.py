@@ -130,6 +130,24 @@ def test_outputs_are_the_rounded_exact_ones_but_for_few_digits(b, Hq, Hkv, I, n,
     assert (out - want).norm() <= DIGITS * want.norm()
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,I", [(4, 4, 64, 1), (8, 2, 128, 1), (8, 1, 64, 3), (3, 3, 128, 9)])
+def test_single_precision_has_its_digits_in_every_group(Hq, Hkv, d, I):
+    """Groups of very different size: each has the digits that it has among its like, which are the same bits when sizes are powers of two."""
+    gen = torch.Generator("cuda").manual_seed(5)
+    n, scale = 4000, 4 * d ** -0.5
+    q, k, v = normal(gen, 2, I, Hq, d), normal(gen, 2, n, Hkv, d), normal(gen, 2, n, Hkv, d)
+    v[:, 500:] *= 3.0                      # (growing on the way)
+    sizes = torch.tensor([2.0 ** -8, 2.0 ** 8, 2.0 ** -3, 1.0] if d == 128 else [2.0 ** 8, 2.0 ** -8], device="cuda").repeat_interleave(32)
+    outs = []
+    for by in (torch.ones_like(sizes), sizes):
+        cache = make(2, Hq, Hkv, d, n, "f32", queries_max=I, softmax_scale=scale)
+        cache.write(k, v * by)
+        outs.append(cache.attend(q, ints([n, n - 100])))
+    want = exact(q, k, v, [n, n - 100], [0, 0], scale)
+    assert (outs[0].double() - want).norm() <= 2.0 ** -18 * want.norm()
+    assert torch.equal(outs[1], outs[0] * sizes)
+
+
 @pytest.mark.parametrize("Hq,I,dtype", [(4, 1, "bf16"), (8, 1, "bf16"), (2, 9, "bf16"), (4, 1, "f32")])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("size", [2.0 ** 26, 2.0 ** 121])
