@@ -367,10 +367,11 @@ bm_status_t bm_packed_destroy(bm_packed_t* cache); /* frees the host handle only
 bm_status_t bm_packed_write(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const void* k, const void* v,
                             const int64_t* strides, int32_t I, const int32_t* start, const int32_t* counts, void* cuda_stream);
 /* The same from the caches of an evicting handle: the n pairs of every cache of samples from_sample0 .. of from_layer, in storage order,
- * become rows 0 .. n - 1 (n: bm_cache_len; nothing happens where it is 0).  Both handles need the same dtype, head_dim, n_kv_heads and
- * device, else BM_ERR_INVALID; BM_ERR_STATE when the samples of the range hold different n or padding pairs; BM_ERR_CAPACITY when n is
- * above the packed capacity.  The pairs' positions and scores stay in the handle that is read, for which this is a call like its own: ordered
- * on cuda_stream, and not to be made while another thread uses it. */
+ * become rows 0 .. n - 1 (n: bm_cache_len; nothing happens where it is 0).  Samples as many as the handle has, whatever its
+ * max_call_samples, and each as far in its sequence as it may be.  Both handles need the same dtype, head_dim, n_kv_heads and device, else
+ * BM_ERR_INVALID; BM_ERR_STATE when the samples of the range hold different n or padding pairs; BM_ERR_CAPACITY when n is above the packed
+ * capacity.  The pairs' positions and scores stay in the handle that is read, for which this is a call like its own: ordered on cuda_stream,
+ * and not to be made while another thread uses it. */
 bm_status_t bm_packed_write_from(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const bm_cache_t* from,
                                  int32_t from_layer, int32_t from_sample0, void* cuda_stream);
 

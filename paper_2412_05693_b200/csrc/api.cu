@@ -159,15 +159,16 @@ bm_status_t set_device(const bm_cache* c) {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Range checks shared by the per-call entry points; returns the common n of the range in *n.
-bm_status_t check_range(const bm_cache* c, int layer, int sample0, int nsamples, int* n, int* curr) {
+// Range checks shared by the per-call entry points; returns the common n of the range in *n.  rows_only: a call that reads the caches' rows,
+// without the workspace (max_call_samples does not limit it) and without the samples' positions.
+bm_status_t check_range(const bm_cache* c, int layer, int sample0, int nsamples, int* n, int* curr, bool rows_only = false) {
   if (c == nullptr) return BM_ERR_INVALID;
   if (layer < 0 || layer >= c->cfg.n_layers) return BM_ERR_INVALID;
   if (sample0 < 0 || nsamples < 1 || (long long)sample0 + nsamples > c->cfg.batch) return BM_ERR_INVALID;
-  if (nsamples > call_samples(&c->cfg)) return BM_ERR_INVALID;
+  if (!rows_only && nsamples > call_samples(&c->cfg)) return BM_ERR_INVALID;
   const size_t o = (size_t)layer * c->cfg.batch + sample0;
   for (int s = 1; s < nsamples; ++s)
-    if (c->n[o + s] != c->n[o] || c->curr_id[o + s] != c->curr_id[o]) return BM_ERR_STATE;
+    if (c->n[o + s] != c->n[o] || (!rows_only && c->curr_id[o + s] != c->curr_id[o])) return BM_ERR_STATE;
   *n = c->n[o];
   *curr = c->curr_id[o];
   return BM_OK;
@@ -238,7 +239,7 @@ int note_cuda_error(cudaError_t e) { return cuda_fail(e); }
 
 int cache_range_rows(const bm_cache* c, int layer, int sample0, int nsamples, CacheRows* out) {
   int n = 0, curr = 0;
-  if (bm_status_t s = check_range(c, layer, sample0, nsamples, &n, &curr); s != BM_OK) return s;
+  if (bm_status_t s = check_range(c, layer, sample0, nsamples, &n, &curr, true); s != BM_OK) return s;
   ++c->dev_calls;  // a later host-fed call orders its pipeline after what reads the rows
   out->dtype = c->cfg.dtype; out->head_dim = c->cfg.head_dim; out->n_kv_heads = c->cfg.n_kv_heads; out->device = c->cfg.device;
   out->n = n;

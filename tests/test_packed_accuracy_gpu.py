@@ -196,3 +196,29 @@ def test_logits_next_to_the_largest_number_in_blocks(d, size):
     want = exact(q, k, v, lens, [0] * b, d ** -0.5)
     assert out.isfinite().all()
     assert (out.double() - want).norm() <= DIGITS * want.norm()
+
+
+def test_handles_that_take_fewer_samples_per_call_are_packed_at_once():
+    """How many samples a call of the evicting handle may have is a matter of its workspace, which packing does not use; so is how far each
+    sample is in its sequence of the pairs' positions."""
+    gen = torch.Generator("cuda").manual_seed(7)
+    handle = bm.BatchMaxCache(bm.Config(batch=5, n_q_heads=4, n_kv_heads=2, head_dim=64, kv_max=40, block_max=40, max_call_samples=2))
+    rows = [[normal(gen, ns, 40, h, 64).bfloat16() for h in (4, 2, 2)] for ns in (2, 2, 1)]
+    for i, (q, k, v) in enumerate(rows):
+        handle.prefill_block(q, k, v, 0, sample0=2 * i)
+    cache = make(5, 4, 2, 64, 64, "bf16")
+    assert cache.write_from(handle) == 40
+    gk, gv = cache.read(0, 40)
+    same(gk, ref.packed_values(torch.cat([r[1] for r in rows])))
+    same(gv, ref.packed_values(torch.cat([r[2] for r in rows])))
+    q, k, v = (normal(gen, 2, 24, h, 64).bfloat16() for h in (4, 2, 2))
+    handle.prefill_block(q, k, v, 40, sample0=2, evict_to=40)                      # samples 2 and 3 go on
+    assert cache.write_from(handle) == 40
+    for s in range(5):
+        for h in range(2):
+            _, _, kr, vr = handle.export(sample=s, kv_head=h, rows=True)
+            same(cache.read(0, 40)[0][s, :, h], ref.packed_values(kr))
+            same(cache.read(0, 40)[1][s, :, h], ref.packed_values(vr))
+    with pytest.raises(bm.BMError) as e:   # samples that the handle does not have
+        make(6, 4, 2, 64, 64, "bf16").write_from(handle)
+    assert e.value.code == 1
