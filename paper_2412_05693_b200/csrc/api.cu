@@ -12,7 +12,7 @@
 #include "common.cuh"
 
 namespace bm {
-unsigned long long g_launch_count = 0;
+std::atomic<unsigned long long> g_launch_count{0};
 int g_last_prefill_path = 0;
 thread_local int g_last_decode_path = 0;
 
@@ -849,7 +849,7 @@ bm_status_t bm_profile_read(int32_t kernel_class, float* total_ms, int32_t* laun
 
 const char* bm_last_cuda_error(void) { return cudaGetErrorString(g_last_cuda_error); }
 
-uint64_t bm_kernel_launch_count(void) { return (uint64_t)g_launch_count; }
+uint64_t bm_kernel_launch_count(void) { return (uint64_t)g_launch_count.load(std::memory_order_relaxed); }
 int32_t bm_last_prefill_path(void) { return g_last_prefill_path; }
 int32_t bm_last_decode_path(void) { return g_last_decode_path; }
 

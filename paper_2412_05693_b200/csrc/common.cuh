@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "smem_configured.h"
 
 struct bm_cache;   // (api.cu)
@@ -140,9 +142,9 @@ cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 block, si
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-extern unsigned long long g_launch_count;
+extern std::atomic<unsigned long long> g_launch_count;   // (packed handles may be used by several threads)
 extern thread_local int g_last_decode_path;   // (api.cu) what bm_last_decode_path reports
-inline void count_launch(int n = 1) { g_launch_count += (unsigned long long)n; }
+inline void count_launch(int n = 1) { g_launch_count.fetch_add((unsigned long long)n, std::memory_order_relaxed); }
 
 // (api.cu) for the entry points in other files: the status code of a failed launch, and where a handle's rows lie.
 int note_cuda_error(cudaError_t e);

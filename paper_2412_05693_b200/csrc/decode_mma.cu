@@ -690,12 +690,15 @@ cudaError_t launch_g(const CacheView& c, const DecodeArgs& a, cudaStream_t st) {
 }  // namespace
 
 int sm_count() {
-  static int count[64] = {};
+  static std::atomic<int> count[64] = {};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
-  if (count[dev] == 0 && cudaDeviceGetAttribute(&count[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    count[dev] = 148;
-  return count[dev];
+  int n = count[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n = 148;
+    count[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
 }
 
 size_t decode_mma_smem_bytes(int d, int g, int n_rows, int target) {

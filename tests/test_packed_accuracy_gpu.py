@@ -4,6 +4,8 @@ An output of bf16 is a number near the exact one, rounded: its rounding alone is
 (an error even over a step that is 2^-7 of the power of two below the value), 2.26e-3.  Where weights go through fp16, once or twice,
 each adds 2^-11 / sqrt(3) of the value at most, 2.8e-4, independent from row to row.  Together 2.3e-3: DIGITS allows 2.5e-3.
 """
+import threading
+
 import pytest
 import torch
 
@@ -222,3 +224,35 @@ def test_handles_that_take_fewer_samples_per_call_are_packed_at_once():
     with pytest.raises(bm.BMError) as e:   # samples that the handle does not have
         make(6, 4, 2, 64, 64, "bf16").write_from(handle)
     assert e.value.code == 1
+
+
+def test_one_cache_used_by_several_threads():
+    gen = torch.Generator("cuda").manual_seed(8)
+    cache = make(2, 8, 2, 128, 600, "bf16")
+    k, v = normal(gen, 2, 600, 2, 128).bfloat16(), normal(gen, 2, 600, 2, 128).bfloat16()
+    cache.write(k, v)
+    lens = ints([600, 431])
+    q = [normal(gen, 2, 1, 8, 128).bfloat16() for _ in range(4)]
+    want = [cache.attend(x, lens) for x in q]
+    spaces, streams = [cache.new_workspace() for _ in q], [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    calls, bad, go = 1500, [], threading.Barrier(len(q))
+
+    def work(i):
+        with torch.cuda.stream(streams[i]):
+            out = torch.empty_like(q[i])
+            go.wait()
+            for _ in range(calls):
+                cache.attend(q[i], lens, out=out, workspace=spaces[i])
+            streams[i].synchronize()
+            if not torch.equal(out, want[i]):
+                bad.append(i)
+
+    before = bm.kernel_launch_count()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(q))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+    assert bm.kernel_launch_count() - before == 2 * calls * len(q)   # the attention, and the joining of its shares
