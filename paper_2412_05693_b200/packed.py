@@ -166,6 +166,8 @@ class PackedCache:
              stream=None):
         """(k, v), each (ns, rows, Hkv, d): what rows row0 .. stand for, zeros at and past lens[s]."""
         ns = self.cfg.batch - sample0 if nsamples is None else nsamples
+        if not (0 <= row0 < row0 + rows <= self.cfg.capacity and 0 <= sample0 < sample0 + ns <= self.cfg.batch):
+            _check(1, "bm_packed_read")   # (before memory is taken for them)
         if stream is None and out is None and self._fast is not None:
             got = self._fast.packed_read(*self._fast_read, row0, rows, layer, sample0, ns, lens)
             if got is not None:

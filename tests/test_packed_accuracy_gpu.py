@@ -256,3 +256,18 @@ def test_one_cache_used_by_several_threads():
         t.join()
     assert not bad
     assert bm.kernel_launch_count() - before == 2 * calls * len(q)   # the attention, and the joining of its shares
+
+
+def test_rows_beyond_the_cache_are_refused_before_memory_is_taken():
+    cache = make(2, 2, 2, 64, 100, "bf16")
+    cache.read(0, 1)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    held = torch.cuda.memory_allocated()
+    for args, kw in [((0, 2 ** 31 - 1), {}), ((1, 2 ** 31 - 1), {}), ((2 ** 31 - 1, 2 ** 31 - 1), {}), ((0, 10 ** 7), dict(stream=torch.cuda.current_stream())),
+                     ((0, 10 ** 7), dict(lens=ints([1, 1]))), ((0, 100), dict(nsamples=10 ** 6)), ((0, 100), dict(nsamples=-1)),
+                     ((0, 100), dict(sample0=3)), ((0, 0), {}), ((0, -5), {}), ((2 ** 40, 1), {})]:
+        with pytest.raises(bm.BMError) as e:
+            cache.read(*args, **kw)
+        assert e.value.code == 1
+    assert torch.cuda.max_memory_allocated() <= held + 4096
