@@ -113,7 +113,8 @@ bm_status_t bm_packed_max_batch(const bm_packed_config_t* cfg, size_t hbm_budget
 }
 
 bm_status_t bm_packed_workspace_bytes(const bm_packed_config_t* cfg, size_t* bytes) {
-  if (!config_ok(cfg, true) || bytes == nullptr) return BM_ERR_INVALID;
+  size_t arena = 0;
+  if (!config_ok(cfg, true) || bytes == nullptr || !arena_size(cfg, &arena)) return BM_ERR_INVALID;
   *bytes = workspace_size(cfg);
   return BM_OK;
 }

@@ -950,8 +950,10 @@ cudaError_t launch_t(const AttendArgs& a, void* workspace, int max_len, cudaStre
 
 size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles) {
   // every run leaves two shares at most; calls of fewer samples, queries or rows take no more runs and no more columns
-  const int64_t cols = (int64_t)queries * g, all = (int64_t)batch * Hkv * ((cols + 3) / 4) * tiles;
-  const int64_t runs = std::min<int64_t>(all, kMostSms * kWarpsPerSm);
+  const int64_t cols = (int64_t)queries * g;
+  int64_t runs = 1;
+  for (const int64_t factor : {(int64_t)batch, (int64_t)Hkv, (cols + 3) / 4, (int64_t)tiles})   // (their product may pass 64 bits)
+    runs = std::min<int64_t>(runs * std::min<int64_t>(factor, kMostSms * kWarpsPerSm), kMostSms * kWarpsPerSm);
   const size_t most = (size_t)runs * 2 * std::min<int64_t>(8, cols) * (d + 4) * sizeof(float);
   return std::max(before_bytes(batch) + most, packed_block_workspace(batch, Hkv));
 }
