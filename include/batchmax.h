@@ -399,6 +399,9 @@ bm_status_t bm_packed_attend(bm_packed_t* cache, int32_t layer, int32_t sample0,
  * BM_ERR_TIMEOUT (a kernel gave up a bounded wait).  bm_packed_clear_status resets it, in stream order. */
 bm_status_t bm_packed_status(bm_packed_t* cache, int32_t* device_status /*HOST out*/, void* cuda_stream);
 bm_status_t bm_packed_clear_status(bm_packed_t* cache, void* cuda_stream);
+/* bm_selftest_wait_timeout for the waits of bm_packed_attend: a warp gives up on copies that nobody issues, bm_packed_status then reports
+ * BM_ERR_TIMEOUT. */
+bm_status_t bm_packed_selftest_wait_timeout(bm_packed_t* cache, void* cuda_stream);
 
 /* ---- per-kernel timing (measurement aid; the paper has no counterpart) ----
  * While enabled, every kernel launch of this library is bracketed by two CUDA events on its stream.

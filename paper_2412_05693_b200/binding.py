@@ -92,6 +92,7 @@ SIGNATURES = {
     "bm_packed_attend": (_i32, [_vp, _i32, _i32, _i32, _vp, _i64p, _i32, _vp, _vp, _i32, _vp, _vp, _sz, _vp]),
     "bm_packed_status": (_i32, [_vp, C.POINTER(_i32), _vp]),
     "bm_packed_clear_status": (_i32, [_vp, _vp]),
+    "bm_packed_selftest_wait_timeout": (_i32, [_vp, _vp]),
     "bm_profile_enable": (_i32, [_i32]),
     "bm_profile_read": (_i32, [_i32, C.POINTER(C.c_float), C.POINTER(_i32)]),
     "bm_kernel_launch_count": (C.c_uint64, []),

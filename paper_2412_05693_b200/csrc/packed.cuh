@@ -88,6 +88,7 @@ struct PackedAttend {
 };
 // Bytes for calls of up to this many samples, kv-heads and queries.
 size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles);
+cudaError_t launch_packed_wait_selftest(int32_t* status, cudaStream_t st);
 extern thread_local int g_last_packed_path;   // (packed_api.cu) what bm_last_packed_path reports
 // (packed_block.cu) the same for blocks of queries, bf16
 size_t packed_block_workspace(int batch, int Hkv);

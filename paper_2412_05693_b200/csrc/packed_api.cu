@@ -245,4 +245,11 @@ bm_status_t bm_packed_clear_status(bm_packed_t* c, void* cuda_stream) {
   return status_of(cudaMemsetAsync(c->status, 0, sizeof(int32_t), static_cast<cudaStream_t>(cuda_stream)));
 }
 
+bm_status_t bm_packed_selftest_wait_timeout(bm_packed_t* c, void* cuda_stream) {
+  if (c == nullptr) return BM_ERR_INVALID;
+  const OnDevice on(c->cfg.device);
+  if (on.err != cudaSuccess) return status_of(on.err);
+  return status_of(launch_packed_wait_selftest(c->status, static_cast<cudaStream_t>(cuda_stream)));
+}
+
 }  // extern "C"

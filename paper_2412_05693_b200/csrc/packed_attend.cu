@@ -96,10 +96,10 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
                ::"r"(tc::smem_u32(dst)), "l"(src), "r"(bytes), "r"(tc::smem_u32(bar)) : "memory");
 }
 // Bounded wait for a slot's copies.  One that gives up records BM_ERR_TIMEOUT; its warp then takes no further tile.
-__device__ __forceinline__ bool slot_full(uint64_t* b, uint32_t parity, int* status) {
+__device__ __forceinline__ bool slot_full(uint64_t* b, uint32_t parity, int* status, int limit = tc::kWaitLimit) {
   const uint32_t addr = tc::smem_u32(b);
 #pragma unroll 1
-  for (int left = tc::kWaitLimit; left > 0; --left) {
+  for (; limit > 0; --limit) {
     uint32_t ok;
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.b32 %0, 1, 0, p;\n}\n"
                  : "=r"(ok) : "r"(addr), "r"(parity), "r"(tc::kWaitSleepNs) : "memory");
@@ -167,6 +167,17 @@ struct Attend {
   static constexpr int kSmem = kWarps * (kWarpBytes + kThirdBytes + kStartBytes);
   static_assert(!PAIR || !kSigned, "");
 };
+
+// Self-test of that wait: a warp waits for copies that nobody issues.
+__global__ void packed_wait_selftest_kernel(int* status) {
+  __shared__ __align__(8) uint64_t bar;
+  if (threadIdx.x == 0) {
+    tc::mbar_init(&bar, 1);
+    tc::mbar_fence_init();
+  }
+  __syncwarp();
+  if (slot_full(&bar, 0, status, 1 << 16)) *status = 0;   // (never)
+}
 
 // The rows of a sample that some query sees: tiles first .. first + n - 1 of its caches.
 struct Tiles {
@@ -947,6 +958,12 @@ cudaError_t launch_t(const AttendArgs& a, void* workspace, int max_len, cudaStre
 }
 
 }  // namespace
+
+cudaError_t launch_packed_wait_selftest(int32_t* status, cudaStream_t st) {
+  packed_wait_selftest_kernel<<<1, 32, 0, st>>>(status);
+  count_launch();
+  return cudaGetLastError();
+}
 
 size_t packed_attend_workspace(int d, int batch, int Hkv, int g, int queries, int tiles) {
   // every run leaves two shares at most; calls of fewer samples, queries or rows take no more runs and no more columns

@@ -220,3 +220,7 @@ class PackedCache:
 
     def clear_status(self, stream=None):
         _check(lib().bm_packed_clear_status(self.h, self._stream(stream)), "bm_packed_clear_status")
+
+    def selftest_wait_timeout(self, stream=None):
+        """Enqueue a warp whose bounded wait runs out: status() is 6 afterwards, until clear_status()."""
+        _check(lib().bm_packed_selftest_wait_timeout(self.h, self._stream(stream)), "bm_packed_selftest_wait_timeout")

@@ -271,3 +271,15 @@ def test_rows_beyond_the_cache_are_refused_before_memory_is_taken():
             cache.read(*args, **kw)
         assert e.value.code == 1
     assert torch.cuda.max_memory_allocated() <= held + 4096
+
+
+def test_a_wait_that_runs_out_is_reported_and_harms_nothing():
+    gen = torch.Generator("cuda").manual_seed(11)
+    cache = make(2, 4, 2, 64, 100, "bf16")
+    k, q, lens = normal(gen, 2, 100, 2, 64).bfloat16(), normal(gen, 2, 1, 4, 64).bfloat16(), ints([100, 60])
+    cache.write(k, k)
+    want = cache.attend(q, lens)
+    cache.selftest_wait_timeout()
+    assert cache.status() == 6
+    cache.clear_status()
+    assert torch.equal(cache.attend(q, lens), want) and cache.status() == 0
