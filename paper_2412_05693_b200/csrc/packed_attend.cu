@@ -778,9 +778,9 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
     for (int t = at.t; t < at.t + share; ++t) {
       if (!slot_full(bar + slot, parity, a.c.status)) {   // gave up: what is in flight lands first, then the warp ends
 #pragma unroll 1
-        for (int k = 1; k < min(kStages, left - (t - at.t)); ++k) {
-          if (++slot == kStages) { slot = 0; parity ^= 1; }
+        for (int k = 0; k < min(kStages, left - (t - at.t)); ++k) {   // (this slot's copy among them)
           slot_full(bar + slot, parity, a.c.status);
+          if (++slot == kStages) { slot = 0; parity ^= 1; }
         }
         return;
       }
