@@ -51,8 +51,9 @@ constexpr int kMostSms = 148;                 // that the workspace is sized for
 constexpr int kFullShift = 12;
 // Queries as integers: a row whose largest element is more than this many times the mean of its magnitudes (3.6 for normal values) gets a
 // third number of 8 bits.  Without it an element is off by 2^-14 of the largest at most, so by 2^-11 of the mean: what fp16 does to weights.
-// For such rows a tile costs 8 more MMAs, on a way of their own.  (Three numbers for every row: 384 samples of 1535 rows, 32 / 8 heads,
-// d = 128, 127 us, two 117, two with this way beside them 119; d = 64 97, 94, 94.)
+// Measured (us; 384 samples of 1535 rows, 32 / 8 heads, d = 128 | 96 of 4096, 64 / 16, d = 64): two numbers 117 | 94, this 118 | 95 and 167 | 139
+// where every tile of queries has such a row, three for every row 127 | 97.  With both halves of a tile side by side on the way of such rows
+// 121 | 94 and 148 | 118.
 constexpr float kUneven = 8.f;
 
 __device__ __forceinline__ void mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1, const float* c) {
@@ -663,23 +664,36 @@ __global__ void __launch_bounds__(kWarps * 32, Attend<T, D, PAIR>::kResident / k
       if (__any_sync(0xffffffffu, grown)) {
         if constexpr (PAIR) {
           if (third) {   // (rare: what this needs is fetched again, so that nothing is kept for it)
-#pragma unroll 1
-            for (int i = 0; i < 2 * G; ++i) {
-              const int sub = i / G, gi = i % G, key = sub * 16 + r / 2 + 4 * (r % 2);
-              uint32_t w0, w1;
-              lds<1>(in + key * (D / 2) + (c * G + gi) * 4, &w0);
-              lds<1>(in + (key + 8) * (D / 2) + (c * G + gi) * 4, &w1);
-              const uint32_t a0[4] = {w0 & 0x0f0f0f0fu, w1 & 0x0f0f0f0fu, w0 >> 4 & 0x0f0f0f0fu, w1 >> 4 & 0x0f0f0f0fu};
-              int acc[4];
-              const uint32_t from = (uint32_t)*third_at(2 * G + gi), start3[4] = {from, 0u, from, 0u};
-              mma_u8s8(acc, a0, (uint32_t)*third_at(gi * 2), (uint32_t)*third_at(gi * 2 + 1), start3);
-              const __half* sc = reinterpret_cast<const __half*>(in + L::kKeyScales) + key * G + gi;
-              // (hidden logits stay -inf, whatever the row's scale)
+            uint32_t low[2 * G], from[G];
 #pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float d = __half2float(sc[8 * G * k]) * (0x1p-8f * (float)acc[2 * k]);
-                if (sub == 0 && s[0][k][0] != -INFINITY) s[0][k][0] += d;
-                if (sub == 1 && s[1][k][0] != -INFINITY) s[1][k][0] += d;
+            for (int i = 0; i < 2 * G; i += 4) lds<4>(third_at(i), low + i);
+            lds<G>(third_at(2 * G), from);
+#pragma unroll 1   // (unrolled it costs the other rows registers)
+            for (int sub = 0; sub < 2; ++sub) {
+              const int key = sub * 16 + r / 2 + 4 * (r % 2);
+              uint32_t w0[G], w1[G], sc[2][G / 2];
+              lds<G>(in + key * (D / 2) + c * 4 * G, w0);
+              lds<G>(in + (key + 8) * (D / 2) + c * 4 * G, w1);
+              lds<G / 2>(in + L::kKeyScales + key * G * 2, sc[0]);
+              lds<G / 2>(in + L::kKeyScales + (key + 8) * G * 2, sc[1]);
+              float d0 = 0.f, d1 = 0.f;
+#pragma unroll
+              for (int gi = 0; gi < G; ++gi) {
+                const uint32_t a0[4] = {w0[gi] & 0x0f0f0f0fu, w1[gi] & 0x0f0f0f0fu, w0[gi] >> 4 & 0x0f0f0f0fu, w1[gi] >> 4 & 0x0f0f0f0fu};
+                const uint32_t from8[4] = {from[gi], 0u, from[gi], 0u};
+                int acc[4];
+                mma_u8s8(acc, a0, low[2 * gi], low[2 * gi + 1], from8);
+                const float2 p0 = unpack(sc[0][gi / 2]), p1 = unpack(sc[1][gi / 2]);
+                d0 = fmaf(gi % 2 ? p0.y : p0.x, (float)acc[0], d0);
+                d1 = fmaf(gi % 2 ? p1.y : p1.x, (float)acc[2], d1);
+              }
+              // (hidden logits stay -inf, whatever the row's scale)
+              if (sub == 0) {
+                if (s[0][0][0] != -INFINITY) s[0][0][0] = fmaf(d0, 0x1p-8f, s[0][0][0]);
+                if (s[0][1][0] != -INFINITY) s[0][1][0] = fmaf(d1, 0x1p-8f, s[0][1][0]);
+              } else {
+                if (s[1][0][0] != -INFINITY) s[1][0][0] = fmaf(d0, 0x1p-8f, s[1][0][0]);
+                if (s[1][1][0] != -INFINITY) s[1][1][0] = fmaf(d1, 0x1p-8f, s[1][1][0]);
               }
             }
             top[0] = fmaxf(fmaxf(s[0][0][0], s[0][1][0]), fmaxf(s[1][0][0], s[1][1][0])) * colmul[0];
