@@ -390,7 +390,16 @@ bm_status_t bm_packed_read(bm_packed_t* cache, int32_t layer, int32_t sample0, i
  *   max_len  the largest length to expect: what the work is split by, results need not have it right; 0 for the capacity
  *   out      DEVICE [nsamples][I][Hq][d], cfg.dtype, contiguous
  *   workspace  DEVICE, 16-byte aligned, >= bm_packed_workspace_bytes (BM_ERR_OOM)
- * Results are the same from run to run; how sums are split, and so their rounding, depends on nsamples, I and max_len. */
+ * Results are the same from run to run; how sums are split, and so their rounding, depends on nsamples, I and max_len.  Rows that no query
+ * of the call sees change no bit of them.
+ * Accuracy.  Maxima and sums are fp32.
+ *   bf16  A logit errs by 2^-16 of scale * sum over the groups of (sum |q|) * (largest |k|) at most.  Calls with up to four query rows per
+ *         cache round queries to integers beside that: an element is off by 2^-11 of its row's mean magnitude at most or, where the row's
+ *         largest is above 8 times the mean, by 2^-21 of the largest.  Weights are rounded to fp16, outside of blocks once more when
+ *         multiplied by a value's scale: 11 bits, in steps of 2^-36 of the row's largest weight at least (2^-24 in blocks; twice that for
+ *         every power of two by which a value scale passes 2).
+ *   fp32  Queries and weights have 22 bits, and so have weights times scales, in steps of 2^-36 of the largest such product of the group of
+ *         elements so far. */
 bm_status_t bm_packed_attend(bm_packed_t* cache, int32_t layer, int32_t sample0, int32_t nsamples, const void* q, const int64_t* strides,
                              int32_t I, const int32_t* lens, const int32_t* first, int32_t max_len, void* out, void* workspace,
                              size_t workspace_bytes, void* cuda_stream);

@@ -4,8 +4,8 @@
 //     O^T = V^T P^T        A = codes of 16 elements x 16 keys, B = weights (16 keys x 8 columns)
 // on warp-level MMAs with fp32 sums.  Rows are read once, 9 bytes for 16 elements, so a step of one token is bound by HBM as long as
 // unpacking keeps up, which is what everything here is about.  (Cycles a scheduler needs per operation, measured: logic on 32 bits, byte
-// permutations, conversions and fp16 arithmetic 2; mma.m16n8k16 of fp16 and mma.m16n8k32 of 8-bit integers 8; the latter of e4m3, which the
-// compiler makes of conversions and fp16 MMAs, 34; ex2 8.)
+// permutations, conversions and fp16 arithmetic 2; mma.m16n8k16 of fp16 and mma.m16n8k32 of 8-bit integers 8; the latter of e4m3 34, so
+// that it seems to be made of conversions and fp16 MMAs; ex2 8.)
 //
 // Unpacking: the code + 8 is an integer u of 4 bits.  The word AND 0x000f000f holds two of them as the fp16 pair (u, u) * 2^-24
 // (subnormals, which the multiplication takes as they are), AND 0x00f000f0 two as u * 2^-20; a shift by 8 gives the other four.  AND
@@ -21,20 +21,22 @@
 // Numbers: a query row is brought to a largest magnitude of 2^13 .. 2^14 by a power of two for the integers (an element is off by 1/2 at
 // most, by 1/256 with the third number), of 2^14 .. 2^15 for fp16, where bf16 values are exact (fp32: two numbers, 22 bits).  Weights are
 // p * 2^shift (fp16, 11 bits; two numbers for fp32) times the value's scale; shift is 12, less where a scale of 2 or more would pass fp16
-// (fp32: it stays, and a group's scales are taken times 2^lift, so that the largest of a group so far is where it keeps both numbers).  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.  Softmax
-// statistics and all sums are fp32.
+// (fp32: it stays, and a group's scales are taken times 2^lift, so that the largest of a group so far is where it keeps both numbers).  Only
+// rows that some query of the tile sees count there.  The maximum that p refers to follows when logits pass it by 2 (in log2), not sooner.
+// Softmax statistics and all sums are fp32.
 //
 // Work: the tiles of all caches of the call, one after another, are cut into equal runs, so that samples of unequal length cost no idle
 // SMs and few long caches are shared by all.  A run is one warp's, which streams it through a ring of shared memory (one
 // cp.async.bulk and one mbarrier per tile) and waits for nobody.  A cache that lies in one run is written out by its warp; of the others
 // the sums go to the workspace, and packed_combine_kernel joins them.
 //
-// Measured (us, both kernels; share of the copy bandwidth over the rows' bytes): d = 128, bf16, 384 samples of 1535 rows, 8 kv-heads, 8
-// query heads 111 (94 %), 32 117 (89 %), 64 134 (77 %); 32 samples of 2048, 40 heads without groups 65 (89 %); one sample of 131072
-// 34 (67 %); 16 of 4096 20 (57 %); 16 of 1472 13.4; one of 1024 7.6.  d = 64, 96 samples of 4096, 64 / 16 heads 92 (75 %).  fp32, 8 samples of
-// 8192, 32 / 8 heads 35 (33 %).  What bounds it: bytes in the first case (437 instructions per 32 rows, schedulers 55 % busy); the
-// instructions with eight columns, at d = 64 and in fp32 (two MMAs and two weights for one); below a few thousand rows the way in (2 us
-// until a warp knows its run, 1 to 3 until its queries are ready) and out (5 us with packed_combine_kernel).
+// Measured in bursts (us, both kernels; share of the copy bandwidth over the rows' bytes; seconds of such calls meet the power limit and
+// take 10 to 20 % more): d = 128, bf16, 384 samples of 1535 rows, 8 kv-heads, 8 query heads 113 (92 %), 32 118 (88 %), 64 135 (77 %); 32
+// samples of 2048, 40 heads without groups 66 (87 %); one sample of 131072 35 (67 %); 16 of 4096 21 (55 %); 16 of 1472 14; one of 1024 7.4.
+// d = 64, 96 samples of 4096, 64 / 16 heads 94 (73 %).  fp32, 8 samples of 8192, 32 / 8 heads 36 (32 %).  What bounds it: bytes in the first
+// case (433 instructions per 32 rows, schedulers 54 % busy); the instructions with eight columns, at d = 64 and in fp32 (two MMAs and two
+// weights for one); below a few thousand rows the way in (2 us until a warp knows its run, 1 to 3 until its queries are ready) and out (5 us
+// with packed_combine_kernel).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

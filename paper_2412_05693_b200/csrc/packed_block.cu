@@ -2,10 +2,11 @@
 // calls whose query rows, I * g of a cache, fill tiles of 128.
 //
 // A CTA has two tiles of 128 query rows of one cache, A and B, and 128 keys at a time.  Eight warps turn the packed rows into fp16 tiles in
-// shared memory (K as code * s, V likewise: 15 bits rounded to 11), one issues S = Q K^T of both, one each O += P V of A and of B, and
-// four softmax warps per tile have a thread for every query row, which also brought its row of Q.  Tensor memory: O_A | O_B | P_A | P_B | S
-// (one of 128 columns that the tiles use in turn at d = 128, one each at d = 64).  A group reads its row's 128 logits into registers at once
-// and gives S back; P has columns of its own, so that the next Q K^T and the P V before run under the exponentials.
+// shared memory (K as code * s, V likewise: exact, since a scale of bf16 rows has 8 bits and a code 3 more; rounded to 11 bits where a scale
+// was held to 65504), one issues S = Q K^T of both, one each O += P V of A and of B, and four softmax warps per tile have a thread for every
+// query row, which also brought its row of Q.  Tensor memory: O_A | O_B | P_A | P_B | S (one of 128 columns that the tiles use in turn at
+// d = 128, one each at d = 64).  A group reads its row's 128 logits into registers at once and gives S back; P has columns of its own, so
+// that the next Q K^T and the P V before run under the exponentials.
 //
 // fp16 has 40 binades: keys and values are taken times a power of two per cache (packed_scales_kernel finds the largest scale), queries per
 // row, and what remains below fp16's smallest is 2^-38 of the largest.  Elements of every eight are kept in the order 0 4 1 5 2 6 3 7, in
@@ -15,12 +16,12 @@
 // values are 0 in the tile, and the first such row of each group is kept: queries see a prefix of the rows, those that see it are NaN there.
 //
 // What bounds it: issue slots and latency of the softmax warps (exponentials 2048 cycles per pair of tiles and scheduler, the tensor pipe as
-// many, of 4400) and, beside them on the same schedulers, the unpacking (a third of the instructions).  Measured, 256 queries of 4 samples
-// over 4352 rows, 32 / 8 heads, d = 128: 89 us, 794 TFLOP/s (128 CTAs, 2.5 us per 128 keys), 16 samples of 4096 332, d = 64 75; one row
-// tile, 32 queries of 16 samples of 4096, 66.  With addresses and scales worked out per element group 93, 345, 75, 69; four unpacking warps
-// with twice the work each (512 threads) 95, 370, 74, 86; those with a mask at the rows' load, which waits for it, 101, 392, 77, 93.
-// 64 keys per step, with logits of its own for either row tile, took 98, 350, 87, 77 where 128 took 94, 349, 74, 69: a step's waits and
-// reductions come twice.  packed_scales_kernel 4.
+// many, of 4400) and, beside them on the same schedulers, the unpacking (a third of the instructions).  Measured in bursts, with
+// packed_scales_kernel (4 us), 256 queries of 4 samples over 4352 rows, 32 / 8 heads, d = 128: 89 us, 793 TFLOP/s (128 CTAs, 2.5 us per 128
+// keys), 16 samples of 4096 336, d = 64 74; one row tile, 32 queries of 16 samples of 4096, 68.  Other ways, before the last of these was
+// found (us, in this order, 89, 331, 75, 66 then): addresses and scales worked out per element group 93, 345, 75, 69; four unpacking warps
+// with twice the work each (512 threads) 95, 370, 74, 86; a mask at the rows' load, which waits for it, 101, 392, 77, 93; 64 keys per step,
+// with logits of its own for either row tile, 98, 350, 87, 77 where 128 took 94, 349, 74, 69: a step's waits and reductions come twice.
 #include <algorithm>
 #include <cmath>
 
@@ -571,12 +572,12 @@ cudaError_t launch_d(const PackedView& c, const PackedAttend& p, cudaStream_t st
 
 // Which calls take this kernel: its time goes by rounds of one CTA per SM, 5 us and so much for 128 keys of one or of two row tiles; that of
 // the warps' kernel by tiles of 32 keys x 8 query rows, shared evenly, and 5 us.  us, this kernel / the other: 32 / 8 heads, d = 128, 16
-// samples of 4096 rows, 32 query rows of a cache 64 / 60, 64 rows 65 / 110, 128 rows 66 / 211; 4 samples, 64 rows 62 / 40, 128 rows 63 / 60,
-// 256 rows 83 / 109, 1024 rows (4352) 89 / 429; 1 sample of 4352, 256 rows 86 / 41, 1024 rows 87 / 114; of 16384, 512 rows 289 / 203; 64
-// samples of 1024, 32 rows 91 / 67, 64 rows 93 / 122; 32 samples of 2048, 32 heads without groups, 32 rows 255 / 239, 64 rows 260 / 425.
-// 8 kv-heads, d = 64, 16 samples of 4096, 32 rows 58 / 43, 64 rows 58 / 73; 4 of 4352, 256 rows 73 / 72, 512 rows 74 / 136; 1, 1024 rows
-// 73 / 70; short caches: 128 samples of 256, d = 128, 64 rows 94 / 86, 128 rows 103 / 162; 40 samples of 400 with 2 heads, d = 64, 257
-// rows 29 / 28.
+// samples of 4096 rows, 32 query rows of a cache 66 / 60, 64 rows 67 / 110, 128 rows 68 / 212; 4 samples, 64 rows 63 / 40, 128 rows 64 / 60,
+// 256 rows 84 / 109, 1024 rows (4352) 89 / 431; 1 sample of 4352, 256 rows 87 / 41, 1024 rows 87 / 114; of 16384, 512 rows 291 / 203; 64
+// samples of 1024, 32 rows 92 / 67, 64 rows 94 / 123; 32 samples of 2048, 32 heads without groups, 32 rows 261 / 223, 64 rows 266 / 430.
+// 8 kv-heads, d = 64, 16 samples of 4096, 32 rows 59 / 45, 64 rows 59 / 74; 4 of 4352, 256 rows 74 / 75, 512 rows 74 / 140; 1, 1024 rows
+// 73 / 72; short caches: 128 samples of 256, d = 128, 64 rows 95 / 87, 128 rows 105 / 163; 40 samples of 400 with 2 heads, d = 64, 257
+// rows 30 / 28.
 bool packed_block_pays(int d, const PackedView& c, int I, int max_len) {
   const double cols = (double)I * c.g, units = (double)c.nsamples * c.Hkv, pairs = std::ceil(cols / (2 * kRows));
   const double step = d == 64 ? (cols <= kRows ? 1.7 : 2.08) : (cols <= kRows ? 1.9 : 2.45);

@@ -4,9 +4,9 @@
 // tile of a cache, whose bytes meet in shared memory, so that global memory sees whole 16-byte pieces although a tile's bytes are ordered for
 // the attention kernel.  A thread has eight consecutive elements of a row, four threads a group.
 //
-// Measured, 16 samples of 4096 rows, 8 heads, d = 128 (344 MB, 52.6 us at the copy bandwidth): bf16 written in 70 us, read in 56; d = 64 77 and
-// 57; fp32, half as many rows, 57 and 51 (46.8).  Reading is bound by HBM, writing bf16 by its instructions (16 per element's lane:
-// schedulers 84 % busy, the logic pipe 70 %); a CTA of 256 threads 77 and 61 (fp32 55 and 49).
+// Measured, 16 samples of 4096 rows, 8 heads, d = 128 (344 MB, 52.6 us at the copy bandwidth): bf16 written in 67 us, read in 57; d = 64, as
+// many bytes, 74 and 58; fp32, half as many rows, 57 and 51 (46.8).  Reading is bound by HBM, writing bf16 by its instructions (16 per
+// element's lane: schedulers 84 % busy, the logic pipe 70 %); with a CTA of 256 threads 77 and 61 where this took 70 and 56 (fp32 55 and 49).
 #include <algorithm>
 
 #include "packed.cuh"
