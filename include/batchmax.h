@@ -393,7 +393,8 @@ bm_status_t bm_packed_read(bm_packed_t* cache, int32_t layer, int32_t sample0, i
  * Results are the same from run to run; how sums are split, and so their rounding, depends on nsamples, I and max_len.  Rows that no query
  * of the call sees change no bit of them.
  * Accuracy.  Maxima and sums are fp32.
- *   bf16  A logit errs by 2^-16 of scale * sum over the groups of (sum |q|) * (largest |k|) at most.  Calls with up to four query rows per
+ *   bf16  A logit errs by 2^-16 of scale * sum over the groups of (sum |q|) * (largest |k|) at most, in blocks by 2^-11 of scale *
+ *         sum |q| |k| over groups whose scale was held to 65504 (keys of 5e5 and more).  Calls with up to four query rows per
  *         cache round queries to integers beside that: an element is off by 2^-11 of its row's mean magnitude at most or, where the row's
  *         largest is above 8 times the mean, by 2^-21 of the largest.  Weights are rounded to fp16, outside of blocks once more when
  *         multiplied by a value's scale: 11 bits, in steps of 2^-36 of the row's largest weight at least (2^-24 in blocks; twice that for
